@@ -177,7 +177,7 @@ def _xent(s):
     picked = z.gather(1, at)
     lse = top + (z - top).exp().sum(1, keepdim=True).log()
     loss = torch.where(counts[:, None], lse - picked, 0.0)
-    out = {"loss": loss[:, 0], "lse": lse[:, 0]}
+    out = {"loss": loss[:, 0], "lse": torch.where(counts, lse[:, 0], 0.0)}     # rows that are ignored have neither
     if s["grads"]:
         p = (z - lse).exp()
         p.scatter_add_(1, at, torch.full_like(picked, -1.0))
@@ -297,7 +297,7 @@ def exact(case, seed):
         keep = (s["targets"] != -100).double()
         row = torch.arange(len(x), device="cuda")
         at = torch.where(s["targets"] == -100, 0, s["targets"])
-        out = {"loss": -logp[row, at] * keep, "lse": lse}
+        out = {"loss": -logp[row, at] * keep, "lse": lse * keep}
         if case["grads"]:
             q = logp.exp_()
             q[row, at] -= 1.0
