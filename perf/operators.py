@@ -17,7 +17,6 @@ BYTES = {"bf16": 2, "fp16": 2, "fp32": 4}
 # AdamW's constants, as training runs use them
 BETA1, BETA2, EPS, DECAY, LR, AT_STEP, SEED = 0.9, 0.95, 1e-8, 0.1, 3e-4, 1000, 12345
 BLOCK = 256             # parameters to a scale of the 8-bit states; every tensor starts on such a block
-E4M3_MAX = 448.0
 
 
 def listed():
@@ -95,6 +94,13 @@ def _tokens(g, n, vocab):
     return ((u * math.log(vocab + 1)).exp().floor().long() - 1).clamp_(0, vocab - 1)
 
 
+def _scale(x):
+    """The power of two of each block by which its largest magnitude comes to lie in (224, 448], 448 being the largest
+    e4m3 value."""
+    top = x.view(-1, BLOCK).abs().amax(1).float().view(torch.int32)
+    return ((((top + 0x1FFFFF) >> 23).clamp(min=9) - 8) << 23).view(torch.float32)
+
+
 def prepare(case, seed):
     g = torch.Generator(device="cuda")
     g.manual_seed(seed)
@@ -131,19 +137,18 @@ def prepare(case, seed):
         param = torch.where(inside, normal(total, std=0.02), 0.0)
         grad = torch.where(inside, normal(total, std=1e-3), 0.0).to(TYPES[case["type"]])
         m = torch.where(inside, normal(total, std=3e-4), 0.0)
-        r = torch.where(inside, normal(total, std=2e-4).abs_().add_(9e-4), 0.0)
+        v = torch.where(inside, normal(total, std=2e-4).abs_().add_(9e-4).square_(), 0.0)
         state.update(param=param, grad=grad, t=AT_STEP)
         # vectors are not decayed
         decay = [DECAY if i == 0 or (i >= 2 and (i - 2) % 5 in (1, 3, 4)) else 0.0 for i in range(len(sizes))]
         blocks = [(n + BLOCK - 1) // BLOCK for n in sizes]
         state["decay"] = torch.tensor(decay, device="cuda").repeat_interleave(torch.tensor(blocks, device="cuda"))
         if case["bits"] == 32:
-            state.update(m=m, v=r * r)
+            state.update(m=m, v=v)
         else:
-            for name, x in (("m", m), ("v", r)):        # the second state's root is what is held in 8 bits
-                scale = x.view(-1, BLOCK).abs().amax(1) / E4M3_MAX
-                y = (x.view(-1, BLOCK) / scale.clamp(min=1e-30)[:, None]).clamp(-E4M3_MAX, E4M3_MAX)
-                state[name] = y.reshape(-1).to(torch.float8_e4m3fn)
+            for name, x in (("m", m), ("v", v)):
+                scale = _scale(x)
+                state[name] = (x.view(-1, BLOCK) / scale[:, None]).reshape(-1).to(torch.float8_e4m3fn)
                 state[name + "_scale"] = scale
         if case["copy"]:
             state["weights"] = param.to(TYPES[case["type"]])
@@ -212,18 +217,16 @@ def _dither(n, t, device):
     return (h & 0xFFFF).int(), (h >> 16).int()
 
 
-def _to_8_bits(x, bits, least):
+def _to_8_bits(x, scale, bits, least):
     """x, in blocks with a scale each, as e4m3 values: dithered by `bits`, so that the mean is x; nonzero values are
     held as one smallest step at least where `least` says so."""
-    x = x.view(-1, BLOCK)
-    scale = x.abs().amax(1) / E4M3_MAX
-    y = torch.where(scale[:, None] > 0, (x.abs() / scale[:, None]), 0.0).clamp(max=E4M3_MAX).reshape(-1)
+    y = (x.abs().view(-1, BLOCK) / scale[:, None]).view(-1)
     fine = ((y.view(torch.int32) + (bits << 4)) & ~0xFFFFF).view(torch.float32)
     steps = (y * 512 + bits.float() * 2.0 ** -16).floor()
     if least:
         steps = torch.where(y > 0, steps.clamp(min=1.0), steps)
     y = torch.where(y < 2.0 ** -6, steps / 512, fine)
-    return torch.copysign(y, x.reshape(-1)).to(torch.float8_e4m3fn), scale
+    return torch.copysign(y, x).to(torch.float8_e4m3fn)
 
 
 def _adamw(s):
@@ -236,19 +239,16 @@ def _adamw(s):
     g, p = s["grad"].float(), s["param"]
     m, v = s["m"], s["v"]
     if s["bits"] == 8:
-        m = (m.float().view(-1, BLOCK) * s["m_scale"][:, None]).view(-1)
-        v = (v.float().view(-1, BLOCK) * s["v_scale"][:, None]).view(-1).square()
+        m, v = ((x.float().view(-1, BLOCK) * scale[:, None]).view(-1) for x, scale in ((m, s["m_scale"]), (v, s["v_scale"])))
     m = m * BETA1 + g * (1 - BETA1)
     v = v * BETA2 + g * g * (1 - BETA2)
-    r = v.sqrt()
     kept = (p.view(-1, BLOCK) * (1 - LR * s["decay"])[:, None]).view(-1)
-    p.copy_(kept - (LR / c1) * (m / (r / math.sqrt(c2) + EPS)))
+    p.copy_(kept - (LR / c1) * (m / (v.sqrt() / math.sqrt(c2) + EPS)))
     if s["bits"] == 8:
         low, high = _dither(p.numel(), s["t"], p.device)
-        for name, x, bits in (("m", m, low), ("v", r, high)):
-            code, scale = _to_8_bits(x, bits, name == "v")
-            s[name].copy_(code)
-            s[name + "_scale"].copy_(scale)
+        for name, x, bits in (("m", m, low), ("v", v, high)):
+            s[name + "_scale"].copy_(_scale(x))
+            s[name].copy_(_to_8_bits(x, s[name + "_scale"], bits, name == "v"))
     else:
         s["m"].copy_(m)
         s["v"].copy_(v)
@@ -316,13 +316,12 @@ def exact(case, seed):
     g, p, m, v = s["grad"].double(), s["param"].double(), s["m"].double(), s["v"].double()
     if case["bits"] == 8:
         m *= s["m_scale"].double().repeat_interleave(BLOCK)
-        v = (v * s["v_scale"].double().repeat_interleave(BLOCK)) ** 2
+        v *= s["v_scale"].double().repeat_interleave(BLOCK)
     m = torch.lerp(g, m, BETA1)
     v = torch.lerp(g ** 2, v, BETA2)
     p = p - LR * s["decay"].double().repeat_interleave(BLOCK) * p
     p = p - LR * (m / (1 - BETA1 ** t)) / ((v / (1 - BETA2 ** t)).sqrt() + EPS)
     out = {"param": p, "m": m, "v": v, "weights": p if case["copy"] else None}
     if case["bits"] == 8:       # which of two neighbouring 8-bit values is held goes by the dithering bits
-        out.update(m=None, v=None, m_scale=m.view(-1, BLOCK).abs().amax(1) / E4M3_MAX,
-                   v_scale=v.sqrt().view(-1, BLOCK).amax(1) / E4M3_MAX)
+        out.update(m=None, v=None, m_scale=_scale(m).double(), v_scale=_scale(v).double())
     return out
