@@ -366,6 +366,96 @@ void guard_destroy(guard_ctx *ctx);
  * guard_create / guard_sweep_qualify when ctx is NULL).  Never NULL. */
 const char *guard_last_error(const guard_ctx *ctx);
 
+/*
+ * Operators of a training step: the load of a node sweep.
+ *
+ * Section 5.2's sweep runs benchmarks on every GPU of a node before guard_sweep_qualify scores their
+ * results; a GPU that passes a plain product or copy may still be slow in the job itself.  These calls are
+ * the parts of a language model's training step that span its vocabulary and its parameters: token
+ * embedding, softmax cross entropy of the vocabulary product, the gradients of both, and the AdamW update.
+ * They load what a step loads (irregular reads, the tensor cores, streaming of all memory) and are ordinary
+ * operators: any caller may train with them.
+ *
+ * Further conventions of these calls
+ *   - No call allocates device memory, synchronises with the host or keeps an address (guard_adamw keeps
+ *     those that it was created with).  All may be captured into a graph, guard_adamw_create and
+ *     guard_adamw_steps excepted.  Calls that may run at the same time need workspaces of their own.
+ *   - d_status: device uint32 or NULL; error bits are OR-ed into it (the caller clears it): 2 = a bounded
+ *     wait ran out (results unspecified), 8 = a token or target outside the table (see each call).
+ *   - Matrices are row-major; a stride is the distance of rows in elements (>= the width).  Outputs are
+ *     contiguous and must not overlap inputs or one another.
+ *   - Sums are held in float32 and every output is rounded once, to nearest.  Results are the same from
+ *     call to call, bit for bit.
+ *   - Sizes of zero are allowed where a call has nothing to do or outputs to clear.
+ */
+enum { GUARD_F32 = 0, GUARD_BF16 = 1, GUARD_F16 = 2 };   /* element types */
+enum { GUARD_STATUS_TIMEOUT = 2, GUARD_STATUS_INDEX = 8 }; /* bits of d_status */
+
+/*
+ * Token embedding: out[i][:] = scale * table[token[i]][:] (one float32 multiply, rounded to dtype).
+ * d_tokens: [tokens] int32 or int64 (token_bits 32 or 64).  d_table: [rows][width], `stride` elements apart,
+ * of type dtype; d_out: [tokens][width] of the same type.  A token outside 0..rows-1 gives a row of NaN and
+ * sets GUARD_STATUS_INDEX.
+ */
+int guard_embed(const void *d_tokens, int token_bits, int64_t tokens, const void *d_table, int64_t rows, int64_t width,
+                int64_t stride, int dtype, float scale, void *d_out, uint32_t *d_status, void *stream);
+
+/*
+ * Gradient of the embedding: dtable[v][:] = scale * sum over i with token[i] = v of grad[i][:], the sum in
+ * float32 over ascending i in a fixed grouping.  Tokens equal to padding_idx add nothing (pass -1 for
+ * none).  accumulate = 0 writes all rows (zero where no token occurs); 1 adds to what d_dtable holds (in
+ * float32, rounded once) and leaves rows without tokens untouched, so that a table tied to the vocabulary
+ * product collects both gradients.  A token outside 0..rows-1 adds nothing and sets GUARD_STATUS_INDEX.
+ * d_grad: [tokens][width], `stride` elements apart, type dtype; d_dtable: [rows][width] of that type.
+ * tokens <= 2^30, rows < 2^31 - 1.
+ */
+size_t guard_embed_grad_workspace_bytes(int64_t tokens, int64_t rows, int64_t width);
+int guard_embed_grad(const void *d_grad, int64_t stride, int dtype, const void *d_tokens, int token_bits, int64_t tokens,
+                     int64_t rows, int64_t width, float scale, int64_t padding_idx, int accumulate, void *d_dtable,
+                     void *d_workspace, size_t workspace_bytes, uint32_t *d_status, void *stream);
+
+/*
+ * AdamW over many tensors in one launch.  Step t of a parameter p with gradient g (all in float32):
+ *   g' = grad_scale * g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2;
+ *   p = p (1 - lr * decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * and, where a copy is asked for, the new p rounded to copy_dtype.
+ *
+ * The states are flat arrays: tensor after tensor, each starting on a block of GUARD_ADAMW_BLOCK elements
+ * (guard_adamw_blocks: blocks in all).  state_bits 32: d_m and d_v are float32.  state_bits 8: d_m and d_v
+ * are 8-bit floats (e4m3), with a float32 scale per block (d_m_scale, d_v_scale): the power of two by which
+ * the block's largest magnitude comes to lie in (224, 448].  Values are rounded up or down at random in
+ * proportion, so that their mean is right: updates smaller than a step of 8 bits would be lost to rounding
+ * to nearest.  The random bits are a function of seed, t and the position alone.  A nonzero v is held as
+ * one smallest step (2^-9 of the scale) at least.  Infinite states become NaN.
+ * Elements behind a tensor's end are left as they are.
+ *
+ * guard_adamw_create copies the table of tensors into the workspace (on `stream`, from host memory; the
+ * addresses must stay valid until guard_adamw_destroy; parameters must not overlap one another).
+ * `step`: updates made so far (0 for new states).  guard_adamw_step makes one update of all tensors and
+ * counts it on the device, so that a captured step counts each replay; lr is taken from d_lr (device, one
+ * float32) where that is not NULL, so that a replay can use another one; d_grad_scale: device, one float32,
+ * or NULL for 1.  guard_adamw_steps reads the counter back (synchronises).  Updates of one object must be
+ * ordered with respect to one another.
+ */
+#define GUARD_ADAMW_BLOCK 256
+typedef struct {
+    float *d_param;       /* [count] float32 */
+    const void *d_grad;   /* [count] of grad_dtype */
+    void *d_copy;         /* [count] of copy_dtype, or NULL */
+    int64_t count;        /* >= 0 */
+    float weight_decay;
+} guard_adamw_tensor;
+typedef struct guard_adamw guard_adamw;
+int64_t guard_adamw_blocks(const guard_adamw_tensor *tensors, int n);
+size_t guard_adamw_workspace_bytes(const guard_adamw_tensor *tensors, int n);
+int guard_adamw_create(guard_adamw **out, const guard_adamw_tensor *tensors, int n, int grad_dtype, int copy_dtype,
+                       int state_bits, double beta1, double beta2, double eps, void *d_m, void *d_v, float *d_m_scale,
+                       float *d_v_scale, int64_t step, uint32_t seed, void *d_workspace, size_t workspace_bytes,
+                       void *stream);
+int guard_adamw_step(guard_adamw *opt, double lr, const float *d_lr, const float *d_grad_scale, void *stream);
+int guard_adamw_steps(guard_adamw *opt, int64_t *steps, void *stream);
+void guard_adamw_destroy(guard_adamw *opt);
+
 /* Host helper: the order-preserving float32 -> uint32 key the kernels select on
  * (total order of finite floats equals unsigned order of keys), and its inverse. */
 uint32_t guard_key_from_float(float x);

@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libguard_b200.so")
 NATIVE = os.path.join(HERE, "_guard_native.so")   # the Python binding's marshalling (csrc/binding.cpp)
-SOURCES = ["guard_api.cu", "xrank.cu", "xrank_bracket.cu", "xrank_cluster.cu", "xrank_split.cu", "xrank_count.cu", "window.cu", "window_bins.cu", "score.cu", "topk.cu", "eval_tail.cu", "sweep.cu", "triage.cu"]
+SOURCES = ["guard_api.cu", "xrank.cu", "xrank_bracket.cu", "xrank_cluster.cu", "xrank_split.cu", "xrank_count.cu", "window.cu", "window_bins.cu", "score.cu", "topk.cu", "eval_tail.cu", "sweep.cu", "triage.cu",
+           "adamw.cu", "embed.cu", "train_api.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "--fmad=false",            # every decision is defined on unfused float32 operations
@@ -61,8 +62,14 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     nvcc = _nvcc()
     extra = ["-Xptxas", "-v"] if verbose else []
 
+    shared = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))]
+    shared += [os.path.join(HERE, "..", "include", "guard_b200.h"), os.path.abspath(__file__)]
+    newest = max(os.path.getmtime(d) for d in shared)
+
     def compile_one(src: str) -> str:
         obj = os.path.join(objdir, src.replace(".cu", ".o"))
+        if not force and not verbose and os.path.exists(obj) and os.path.getmtime(obj) > max(newest, os.path.getmtime(os.path.join(CSRC, src))):
+            return obj      # newer than its source, every header and these flags
         cmd = [nvcc, *NVCC_FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if verbose or r.returncode != 0:

@@ -1,0 +1,271 @@
+"""Binding of the training-step operators of libguard_b200.so: token embedding, softmax cross entropy of a vocabulary
+product, their gradients, and AdamW (the C ABI's last section in include/guard_b200.h).
+
+They are the load of a node sweep (sweep_run.py) and ordinary operators besides.  Argument marshalling only, as in
+guard.py: PyTorch supplies device memory and the current stream, every step runs in the library's kernels, and nothing is
+recorded for autograd: a gradient is a call of its own.
+
+Errors in data (a token outside its table) cannot be raised by the call that meets them without waiting for the GPU: they
+are kept in a status word per device, which sync_status() reads and clears, or in the uint32 tensor that the caller passes
+as out["status"].
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Dict, Optional, Sequence
+
+import torch
+
+from . import guard
+from .guard import GUARD_OK, GuardError
+
+STATUS_TIMEOUT, STATUS_INDEX = 2, 8
+BLOCK = 256                 # elements to a scale of AdamW's 8-bit states; tensors start on such blocks of the flat states
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_TOKENS = {torch.int32: 32, torch.int64: 64}
+
+
+class _AdamwTensor(C.Structure):
+    _fields_ = [("d_param", C.c_void_p), ("d_grad", C.c_void_p), ("d_copy", C.c_void_p), ("count", C.c_int64),
+                ("weight_decay", C.c_float)]
+
+
+_lib = None
+
+
+def lib():
+    """The loaded library with the operators' prototypes (raises if it has not been built)."""
+    global _lib
+    if _lib is None:
+        L = guard.lib()
+        vp, i64, f, d, i, z = C.c_void_p, C.c_int64, C.c_float, C.c_double, C.c_int, C.c_size_t
+        tp = C.POINTER(_AdamwTensor)
+        for name, res, args in (
+                ("guard_embed", i, [vp, i, i64, vp, i64, i64, i64, i, f, vp, vp, vp]),
+                ("guard_embed_grad_workspace_bytes", z, [i64, i64, i64]),
+                ("guard_embed_grad", i, [vp, i64, i, vp, i, i64, i64, i64, f, i64, i, vp, vp, z, vp, vp]),
+                ("guard_adamw_blocks", i64, [tp, i]),
+                ("guard_adamw_workspace_bytes", z, [tp, i]),
+                ("guard_adamw_create", i, [C.POINTER(vp), tp, i, i, i, i, d, d, d, vp, vp, vp, vp, i64, C.c_uint32, vp, z, vp]),
+                ("guard_adamw_step", i, [vp, d, vp, vp, vp]),
+                ("guard_adamw_steps", i, [vp, C.POINTER(i64), vp]),
+                ("guard_adamw_destroy", None, [vp])):
+            fn = getattr(L, name)
+            fn.restype, fn.argtypes = res, args
+        _lib = L
+    return _lib
+
+
+def _check(rc: int) -> None:
+    if rc != GUARD_OK:
+        raise GuardError(rc, lib().guard_last_error(None).decode())
+
+
+def _here(device: torch.device):
+    return guard._HERE_CTX if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _cuda(t: torch.Tensor, what: str, device: Optional[torch.device] = None) -> torch.device:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor" % what)
+    if device is not None and t.device != device:
+        raise ValueError("%s is on %s, the other tensors on %s" % (what, t.device, device))
+    return t.device
+
+
+def _dtype(t: torch.Tensor, what: str) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError("%s must be float32, bfloat16 or float16, got %s" % (what, t.dtype))
+    return code
+
+
+def _rows(t: torch.Tensor, what: str) -> int:
+    """Distance of the rows of a matrix whose rows are contiguous."""
+    if t.dim() != 2:
+        raise ValueError("%s must be a matrix" % what)
+    n, d = t.shape
+    if d > 1 and t.stride(1) != 1 or n > 1 and t.stride(0) < d:
+        raise ValueError("%s must have contiguous rows that do not overlap" % what)
+    return t.stride(0) if n > 1 else d
+
+
+def _contiguous(t: torch.Tensor, what: str, dtype: torch.dtype, numel: int, device: torch.device) -> int:
+    _cuda(t, what, device)
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() != numel:
+        raise ValueError("%s must be contiguous, of %s and of %d elements" % (what, dtype, numel))
+    return t.data_ptr()
+
+
+def _tokens(t: torch.Tensor, device: torch.device) -> int:
+    _cuda(t, "tokens", device)
+    bits = _TOKENS.get(t.dtype)
+    if bits is None or not t.is_contiguous():
+        raise ValueError("tokens must be contiguous, int32 or int64")
+    return bits
+
+
+def _workspace(given: Optional[torch.Tensor], need: int, device: torch.device) -> torch.Tensor:
+    if need == 0:
+        raise GuardError(-1, "invalid sizes")
+    if given is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    _cuda(given, "workspace", device)
+    if given.dtype != torch.uint8 or not given.is_contiguous():
+        raise ValueError("workspace must be contiguous, of torch.uint8")
+    return given
+
+
+_status: Dict[int, torch.Tensor] = {}
+
+
+def _status_ptr(out, device: torch.device) -> int:
+    given = out.get("status") if out is not None else None
+    if given is not None:
+        return _contiguous(given, "status", torch.uint32, 1, device)
+    word = _status.get(device.index)
+    if word is None:
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("make the first call on a device before capturing, or pass out['status']")
+        word = _status[device.index] = torch.zeros(1, dtype=torch.int32, device=device)
+        torch.cuda.current_stream(device).synchronize()      # other streams may use it from now on
+    return word.data_ptr()
+
+
+def sync_status(device=None) -> None:
+    """Waits for the current stream of `device`, raises GuardError if a call before met an error in its data, and clears
+    the device's status word."""
+    index = torch.device(device if device is not None else "cuda").index
+    index = torch.cuda.current_device() if index is None else index
+    word = _status.get(index)
+    if word is None:
+        return
+    with torch.cuda.device(index):
+        bits = int(word.item())
+        if bits:
+            word.zero_()
+            if bits & STATUS_TIMEOUT:
+                raise GuardError(-5, "a bounded wait of an operator ran out: its results are unspecified")
+            raise GuardError(-1, "a token or target lies outside its table")
+
+
+def embed(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.0,
+          out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """out["out"][...] = scale * table[tokens[...]]: rows of table [rows, width], any shape of tokens.  A token outside the
+    table gives a row of NaN."""
+    dev = _cuda(table, "table")
+    bits, code, stride = _tokens(tokens, dev), _dtype(table, "table"), _rows(table, "table")
+    rows, width = table.shape
+    with _here(dev):
+        if out is None:
+            out = {"out": torch.empty((*tokens.shape, width), dtype=table.dtype, device=dev)}
+        to = _contiguous(out["out"], "out", table.dtype, tokens.numel() * width, dev)
+        _check(lib().guard_embed(tokens.data_ptr(), bits, tokens.numel(), table.data_ptr(), rows, width, stride, code, scale, to,
+                                 _status_ptr(out, dev), guard._stream()))
+    return out
+
+
+def embed_grad(grad: torch.Tensor, tokens: torch.Tensor, rows: int, *, scale: float = 1.0, padding_idx: int = -1,
+               accumulate: bool = False, workspace: Optional[torch.Tensor] = None,
+               out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """out["dtable"][v] = scale * sum of grad[i] over tokens[i] == v, [rows, width] of grad's type; with accumulate, added
+    to what out["dtable"] holds (rows without tokens stay as they are).  grad: [tokens, width], or contiguous of
+    [..., width].  Tokens equal to padding_idx add nothing."""
+    dev = _cuda(grad, "grad")
+    if grad.dim() != 2 and grad.dim() > 0 and grad.is_contiguous():
+        grad = grad.view(-1, grad.shape[-1])
+    bits, code, stride = _tokens(tokens, dev), _dtype(grad, "grad"), _rows(grad, "grad")
+    n, width = grad.shape
+    if tokens.numel() != n:
+        raise ValueError("%d gradient rows for %d tokens" % (n, tokens.numel()))
+    with _here(dev):
+        if out is None:
+            if accumulate:
+                raise ValueError("accumulate needs out['dtable']")
+            out = {"dtable": torch.empty((rows, width), dtype=grad.dtype, device=dev)}
+        to = _contiguous(out["dtable"], "dtable", grad.dtype, rows * width, dev)
+        ws = _workspace(workspace, lib().guard_embed_grad_workspace_bytes(n, rows, width), dev)
+        _check(lib().guard_embed_grad(grad.data_ptr(), stride, code, tokens.data_ptr(), bits, n, rows, width, scale, padding_idx,
+                                      1 if accumulate else 0, to, ws.data_ptr(), ws.numel(), _status_ptr(out, dev), guard._stream()))
+    return out
+
+
+class AdamW:
+    """AdamW over many tensors, one launch per step.
+
+    params: contiguous float32 CUDA tensors, updated in place; grads: the buffers that a step reads, one per parameter, all
+    of one type; copies: tensors of one type that receive the new parameters rounded (or None).  The tensors are kept and
+    must not be moved.  weight_decay: a number, or one per tensor.
+
+    state: {"m", "v"} of a flat layout, each parameter starting on a block of 256 elements (numel of a state:
+    256 * state_blocks(params)); float32 for state_bits 32, and for 8 torch.float8_e4m3fn with {"m_scale", "v_scale"}, a
+    float32 per block.  None: zeros.  step: updates made so far.
+    """
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], *, betas=(0.9, 0.999), eps: float = 1e-8,
+                 weight_decay=0.0, state_bits: int = 32, copies: Optional[Sequence[torch.Tensor]] = None,
+                 state: Optional[Dict[str, torch.Tensor]] = None, step: int = 0, seed: int = 0):
+        self._h = C.c_void_p()
+        self.params, self.grads, self.copies = list(params), list(grads), None if copies is None else list(copies)
+        n = len(self.params)
+        if n == 0 or len(self.grads) != n or (self.copies is not None and len(self.copies) != n):
+            raise ValueError("need parameters, and as many gradients and copies")
+        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * n
+        if len(decay) != n:
+            raise ValueError("expected %d weight decays, got %d" % (n, len(decay)))
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        dev = self.device = _cuda(self.params[0], "params")
+        gtype = self.grads[0].dtype
+        ctype = self.copies[0].dtype if self.copies is not None else torch.float32
+        table = (_AdamwTensor * n)()
+        for i, p in enumerate(self.params):
+            t = table[i]
+            t.count, t.weight_decay = p.numel(), decay[i]
+            t.d_param = _contiguous(p, "params", torch.float32, p.numel(), dev)
+            t.d_grad = _contiguous(self.grads[i], "grads", gtype, p.numel(), dev)
+            t.d_copy = _contiguous(self.copies[i], "copies", ctype, p.numel(), dev) if self.copies is not None else None
+        gcode = _dtype(self.grads[0], "grads")
+        ccode = _dtype(self.copies[0], "copies") if self.copies is not None else 0
+        blocks = self.blocks = int(lib().guard_adamw_blocks(table, n))
+        kinds = {"m": (torch.float32, BLOCK), "v": (torch.float32, BLOCK)} if state_bits == 32 else {
+            "m": (torch.float8_e4m3fn, BLOCK), "v": (torch.float8_e4m3fn, BLOCK), "m_scale": (torch.float32, 1), "v_scale": (torch.float32, 1)}
+        with _here(dev):
+            if state is None:
+                state = {k: torch.zeros(blocks * per, dtype=t, device=dev) for k, (t, per) in kinds.items()}
+            at = {k: _contiguous(state[k], "state[%r]" % k, t, blocks * per, dev) for k, (t, per) in kinds.items()}
+            self.state = {k: state[k] for k in kinds}
+            self._ws = torch.empty(max(256, int(lib().guard_adamw_workspace_bytes(table, n))), dtype=torch.uint8, device=dev)
+            _check(lib().guard_adamw_create(C.byref(self._h), table, n, gcode, ccode, state_bits, betas[0], betas[1], eps, at["m"], at["v"],
+                                            at.get("m_scale"), at.get("v_scale"), step, seed & 0xFFFFFFFF, self._ws.data_ptr(),
+                                            self._ws.numel(), guard._stream()))
+
+    @staticmethod
+    def state_blocks(params: Sequence[torch.Tensor]) -> int:
+        return sum((p.numel() + BLOCK - 1) // BLOCK for p in params)
+
+    def step(self, lr, *, grad_scale: Optional[torch.Tensor] = None) -> None:
+        """One update of all parameters.  lr: a number, or a float32 CUDA tensor of one element (which a captured step reads
+        at every replay); grad_scale: such a tensor too, multiplied into the gradients."""
+        with _here(self.device):
+            dlr = _contiguous(lr, "lr", torch.float32, 1, self.device) if isinstance(lr, torch.Tensor) else None
+            gs = _contiguous(grad_scale, "grad_scale", torch.float32, 1, self.device) if grad_scale is not None else None
+            _check(lib().guard_adamw_step(self._h, 0.0 if dlr else lr, dlr, gs, guard._stream()))
+
+    def steps(self) -> int:
+        """Updates made so far (synchronises)."""
+        n = C.c_int64()
+        with _here(self.device):
+            _check(lib().guard_adamw_steps(self._h, C.byref(n), guard._stream()))
+        return n.value
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) and _lib is not None:
+            _lib.guard_adamw_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

@@ -1,0 +1,95 @@
+"""Refusals of the training-step operators, which need no GPU: every call below fails before any CUDA work."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2605_17879_b200 import build as gbuild
+
+P = 256 * 4096          # an address that is never dereferenced
+Q = P + (1 << 40)
+WS = Q + (1 << 40)
+
+
+@pytest.fixture(scope="module")
+def L():
+    gbuild.build_library()
+    from paper_2605_17879_b200 import operators
+    return operators.lib()
+
+
+def text(L):
+    return L.guard_last_error(None).decode()
+
+
+def test_embed_refusals(L):
+    def call(tokens=P, bits=64, n=4, table=Q, rows=8, width=16, stride=16, dtype=1, out=WS):
+        return L.guard_embed(tokens, bits, n, table, rows, width, stride, dtype, 1.0, out, None, None)
+    assert call(n=0) == 0 and call(n=0, tokens=None, out=None) == 0
+    for bad in (dict(bits=16), dict(dtype=3), dict(dtype=-1), dict(n=-1), dict(rows=-1), dict(width=0), dict(stride=15), dict(width=1 << 25, stride=1 << 25),
+                dict(tokens=None), dict(table=None), dict(out=None), dict(tokens=P + 4), dict(table=Q + 1), dict(out=WS + 1), dict(n=1 << 60),
+                dict(out=Q + 32), dict(out=P)):
+        assert call(**bad) == -1, bad
+        assert text(L)
+
+
+def test_embed_grad_refusals(L):
+    need = L.guard_embed_grad_workspace_bytes(100, 50, 16)
+    assert need > 0 and need % 256 == 0
+    for bad in ((-1, 50, 16), (1 << 31, 50, 16), (100, -1, 16), (100, (1 << 31) - 1, 16), (100, 50, 0)):
+        assert L.guard_embed_grad_workspace_bytes(*bad) == 0
+    def call(grad=P, stride=16, dtype=1, tokens=P + (1 << 30), bits=64, n=100, rows=50, width=16, pad=-1, acc=0, out=Q, ws=WS, nws=need):
+        return L.guard_embed_grad(grad, stride, dtype, tokens, bits, n, rows, width, 1.0, pad, acc, out, ws, nws, None, None)
+    assert call(rows=0) == 0 and call(n=0, acc=1) == 0
+    for bad in (dict(bits=8), dict(dtype=7), dict(n=-1), dict(stride=8), dict(width=0), dict(pad=-2), dict(pad=50), dict(grad=None), dict(tokens=None),
+                dict(out=None), dict(grad=P + 1), dict(out=P), dict(out=P + (1 << 30)), dict(out=WS)):
+        assert call(**bad) == -1, bad
+    for bad in (dict(ws=None), dict(ws=WS + 16), dict(nws=need - 1)):
+        assert call(**bad) == -2, bad
+
+
+def test_adamw_refusals(L):
+    from paper_2605_17879_b200 import operators as ops
+    h = C.c_void_p()
+    def call(tensors=((P, Q, None, 1000, 0.1), (P + 4096, Q + 4096, None, 10, 0.0)), n=None, gt=1, ct=1, bits=32, b1=0.9, b2=0.99, eps=1e-8, m=WS,
+             v=WS + (1 << 20), ms=None, vs=None, step=0, ws=WS + (1 << 30), nws=1 << 20):
+        t = (ops._AdamwTensor * max(1, len(tensors)))(*[ops._AdamwTensor(*x) for x in tensors])
+        return L.guard_adamw_create(C.byref(h), t, len(tensors) if n is None else n, gt, ct, bits, b1, b2, eps, m, v, ms, vs, step, 0, ws, nws, None)
+    inf = float("inf")
+    for bad in (dict(n=0), dict(n=-1), dict(gt=3), dict(ct=-1), dict(bits=16), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(b2=float("nan")), dict(eps=-1.0),
+                dict(eps=inf), dict(step=-1), dict(m=None), dict(v=WS + 8), dict(bits=8), dict(tensors=((P, Q, None, -1, 0.0),)), dict(tensors=((None, Q, None, 5, 0.0),)),
+                dict(tensors=((P, None, None, 5, 0.0),)), dict(tensors=((P + 2, Q, None, 5, 0.0),)), dict(tensors=((P, Q + 1, None, 5, 0.0),)),
+                dict(tensors=((P, Q, None, 5, inf),)),
+                dict(tensors=((P, Q, None, 1000, 0.0), (P, Q + 4096, None, 10, 0.0))),              # the same parameter twice
+                dict(tensors=((P, Q, P + 8, 1000, 0.0),)), dict(tensors=((P, P, None, 1000, 0.0),)),  # copy or gradient inside it
+                dict(tensors=((P, Q, Q, 1000, 0.0),)), dict(m=P), dict(v=WS), dict(ws=WS)):
+        assert call(**bad) == -1, bad
+        assert h.value is None
+    for bad in (dict(ws=None), dict(ws=WS + (1 << 30) + 8), dict(nws=300)):
+        assert call(**bad) == -2, bad
+    t = (ops._AdamwTensor * 3)(ops._AdamwTensor(P, Q, None, 0, 0.0), ops._AdamwTensor(P, Q, None, 257, 0.0), ops._AdamwTensor(P, Q, None, 256, 0.0))
+    assert L.guard_adamw_blocks(t, 3) == 3 and L.guard_adamw_blocks(t, 0) == 0 and L.guard_adamw_blocks(None, 1) == -1
+    assert L.guard_adamw_step(None, 1e-3, None, None, None) == -1
+    assert L.guard_adamw_steps(None, None, None) == -1
+    L.guard_adamw_destroy(None)
+
+
+def test_binding_refusals(L):
+    from paper_2605_17879_b200 import operators as ops
+    x = torch.zeros(4, 8)
+    ids = torch.zeros(4, dtype=torch.int64)
+    with pytest.raises(ValueError):
+        ops.embed(ids, x)                       # CPU tensors
+    with pytest.raises(ValueError):
+        ops.embed_grad(x, ids, 4)
+    with pytest.raises(ValueError):
+        ops.AdamW([x], [x])
+    with pytest.raises(ValueError):
+        ops.AdamW([], [])
+    with pytest.raises(ValueError):
+        ops.AdamW([x], [x], state_bits=16)
+    for bad in (torch.zeros(8, 8)[:, ::2], torch.zeros(8).expand(4, 8), torch.zeros(8)):
+        with pytest.raises(ValueError):
+            ops._rows(bad, "table")
+    assert ops._rows(torch.zeros(8, 8)[:, :5], "table") == 8 and ops._rows(torch.zeros(1, 5).expand(1, 5), "table") == 5
+    assert ops.AdamW.state_blocks([torch.zeros(0), torch.zeros(257)]) == 2
