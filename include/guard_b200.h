@@ -415,6 +415,32 @@ int guard_embed_grad(const void *d_grad, int64_t stride, int dtype, const void *
                      void *d_workspace, size_t workspace_bytes, uint32_t *d_status, void *stream);
 
 /*
+ * Softmax cross entropy of a vocabulary product, without keeping the logits: with z = x w^T in float32,
+ *   lse[n] = log sum over v of exp(z[n][v]);  loss[n] = lse[n] - z[n][target[n]].
+ * d_x: [rows][width], d_w: [vocab][width], of type dtype (GUARD_BF16 or GUARD_F16), 16-byte aligned, strides
+ * multiples of 8 elements, width a multiple of 8.  d_targets: [rows] int32 or int64 (target_bits).  Rows whose
+ * target is ignore_index are left out: loss and lse are 0, and what they hold reaches nothing.  A target
+ * that is neither ignore_index nor in 0..vocab-1 sets GUARD_STATUS_INDEX, gives a loss of NaN and an lse of 0,
+ * and is left out of the gradients.  Logits that are not finite give losses and gradients that are not.
+ *
+ * guard_linear_xent_grad: the gradients of sum over n of grad_loss[n] * loss[n]: with
+ *   G[n][v] = grad_loss[n] * (exp(z[n][v] - lse[n]) - [v = target[n]]),
+ *   dx = G w, [rows][width], and dw = G^T x, [vocab][width], both of type dtype.
+ * d_lse: as guard_linear_xent gave it.  d_grad_loss: [rows] (grad_stride 1) or one value for all rows
+ * (grad_stride 0).  One of d_dx and d_dw may be NULL.  G is held in dtype, a piece of the vocabulary at a time.
+ * The workspace depends on whether gradients are wanted (grads 0 or 1).
+ */
+size_t guard_linear_xent_workspace_bytes(int64_t rows, int64_t width, int64_t vocab, int grads);
+int guard_linear_xent(const void *d_x, int64_t x_stride, const void *d_w, int64_t w_stride, int64_t rows, int64_t width,
+                      int64_t vocab, int dtype, const void *d_targets, int target_bits, int64_t ignore_index,
+                      float *d_loss, float *d_lse, void *d_workspace, size_t workspace_bytes, uint32_t *d_status,
+                      void *stream);
+int guard_linear_xent_grad(const void *d_x, int64_t x_stride, const void *d_w, int64_t w_stride, int64_t rows, int64_t width,
+                           int64_t vocab, int dtype, const void *d_targets, int target_bits, int64_t ignore_index,
+                           const float *d_lse, const float *d_grad_loss, int grad_stride, void *d_dx, void *d_dw,
+                           void *d_workspace, size_t workspace_bytes, uint32_t *d_status, void *stream);
+
+/*
  * AdamW over many tensors in one launch.  Step t of a parameter p with gradient g (all in float32):
  *   g' = grad_scale * g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2;
  *   p = p (1 - lr * decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libguard_b200.so")
 NATIVE = os.path.join(HERE, "_guard_native.so")   # the Python binding's marshalling (csrc/binding.cpp)
 SOURCES = ["guard_api.cu", "xrank.cu", "xrank_bracket.cu", "xrank_cluster.cu", "xrank_split.cu", "xrank_count.cu", "window.cu", "window_bins.cu", "score.cu", "topk.cu", "eval_tail.cu", "sweep.cu", "triage.cu",
-           "adamw.cu", "embed.cu", "train_api.cu"]
+           "adamw.cu", "embed.cu", "xent.cu", "train_api.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "--fmad=false",            # every decision is defined on unfused float32 operations

@@ -129,6 +129,100 @@ int guard_embed_grad(const void *d_grad, int64_t stride, int dtype, const void *
     return launched(launch_embed_grad(a, dtype, (cudaStream_t)stream), "embedding gradient");
 }
 
+size_t guard_linear_xent_workspace_bytes(int64_t rows, int64_t width, int64_t vocab, int grads) {
+    if (rows < 1 || rows > (1LL << 30) || width < 8 || width > (1 << 24) || width % 8 || vocab < 1 || vocab > (1LL << 30)) return 0;
+    // tiles are counted in 32 bits (at most 148 splits of the depth)
+    if (((rows + 127) / 128) * ((vocab + 255) / 256) > (1LL << 30) || ((rows + 127) / 128) * ((width + 255) / 256) > (1LL << 23) ||
+        ((vocab + 127) / 128) * ((width + 255) / 256) > (1LL << 30))
+        return 0;
+    return xent_workspace(rows, width, vocab, grads != 0);
+}
+
+// The checks that both directions share; 0 or an error.
+static int xent_check(const XentArgs &a, size_t need, size_t given, const void *out0, size_t n0, const void *out1, size_t n1) {
+    if ((a.dtype != GUARD_BF16 && a.dtype != GUARD_F16) || (a.target_bits != 32 && a.target_bits != 64))
+        return call_error(GUARD_ERR_ARG, "dtype must be GUARD_BF16 or GUARD_F16, target_bits 32 or 64");
+    if (need == 0 || a.x_stride < a.width || a.w_stride < a.width || a.x_stride % 8 || a.w_stride % 8 || a.x_stride >= (1LL << 36) || a.w_stride >= (1LL << 36))
+        return call_error(GUARD_ERR_ARG, "invalid sizes: need 1 <= vocab <= 2^30, rows <= 2^30, width a multiple of 8 up to 2^24, strides multiples of 8 and >= width, and a product that tiles");
+    if (!a.x || !a.w || !a.targets) return call_error(GUARD_ERR_ARG, "d_x, d_w or d_targets is NULL");
+    if (!on(a.x, 16) || !on(a.w, 16) || !on(a.targets, a.target_bits / 8)) return call_error(GUARD_ERR_ARG, "d_x and d_w must be 16-byte aligned, d_targets to its elements");
+    if (!a.workspace || !on(a.workspace, 256) || given < need)
+        return call_error(GUARD_ERR_WORKSPACE, "workspace must be non-NULL, 256-byte aligned and at least %zu bytes", need);
+    const struct { const void *p; size_t n; } ins[] = {{a.x, ((size_t)(a.rows - 1) * a.x_stride + a.width) * 2}, {a.w, ((size_t)(a.vocab - 1) * a.w_stride + a.width) * 2},
+                                                       {a.targets, (size_t)a.rows * a.target_bits / 8}, {a.workspace, need},
+                                                       {a.lse, (size_t)a.rows * 4}, {a.grad_loss, a.grad_stride ? (size_t)a.rows * 4 : 4}};
+    for (const auto &in : ins)
+        if (in.p && (overlap(out0, out0 ? n0 : 0, in.p, in.n) || overlap(out1, out1 ? n1 : 0, in.p, in.n))) return call_error(GUARD_ERR_ARG, "an output overlaps an input or the workspace");
+    if (out0 && out1 && overlap(out0, n0, out1, n1)) return call_error(GUARD_ERR_ARG, "the outputs overlap");
+    return GUARD_OK;
+}
+
+int guard_linear_xent(const void *d_x, int64_t x_stride, const void *d_w, int64_t w_stride, int64_t rows, int64_t width,
+                      int64_t vocab, int dtype, const void *d_targets, int target_bits, int64_t ignore_index,
+                      float *d_loss, float *d_lse, void *d_workspace, size_t workspace_bytes, uint32_t *d_status,
+                      void *stream) {
+    if (rows == 0 && vocab >= 1 && width >= 8 && width % 8 == 0) return GUARD_OK;
+    XentArgs a{};
+    a.x = d_x;
+    a.w = d_w;
+    a.rows = rows;
+    a.width = width;
+    a.vocab = vocab;
+    a.x_stride = x_stride;
+    a.w_stride = w_stride;
+    a.dtype = dtype;
+    a.targets = d_targets;
+    a.target_bits = target_bits;
+    a.ignore = ignore_index;
+    a.loss = d_loss;
+    a.lse_out = d_lse;
+    a.workspace = d_workspace;
+    a.status = d_status;
+    if (!d_loss || !d_lse || !on(d_loss, 4) || !on(d_lse, 4)) return call_error(GUARD_ERR_ARG, "d_loss and d_lse must be non-NULL and aligned to their elements");
+    const int rc = xent_check(a, guard_linear_xent_workspace_bytes(rows, width, vocab, 0), workspace_bytes, d_loss, (size_t)rows * 4, d_lse, (size_t)rows * 4);
+    if (rc != GUARD_OK) return rc;
+    return launched(launch_xent(a, (cudaStream_t)stream), "cross entropy");
+}
+
+int guard_linear_xent_grad(const void *d_x, int64_t x_stride, const void *d_w, int64_t w_stride, int64_t rows, int64_t width,
+                           int64_t vocab, int dtype, const void *d_targets, int target_bits, int64_t ignore_index,
+                           const float *d_lse, const float *d_grad_loss, int grad_stride, void *d_dx, void *d_dw,
+                           void *d_workspace, size_t workspace_bytes, uint32_t *d_status, void *stream) {
+    if (grad_stride != 0 && grad_stride != 1) return call_error(GUARD_ERR_ARG, "grad_stride must be 0 or 1");
+    if (!d_dx && !d_dw) return call_error(GUARD_ERR_ARG, "d_dx and d_dw are both NULL");
+    if (!on(d_dx, 16) || !on(d_dw, 16)) return call_error(GUARD_ERR_ARG, "d_dx and d_dw must be 16-byte aligned");
+    if (rows == 0 && vocab >= 1 && width >= 8 && width % 8 == 0 && (dtype == GUARD_BF16 || dtype == GUARD_F16)) {
+        if (!d_dw) return GUARD_OK;
+        const cudaError_t e = cudaMemsetAsync(d_dw, 0, (size_t)vocab * width * 2, (cudaStream_t)stream);
+        if (e == cudaSuccess) return GUARD_OK;
+        (void)cudaGetLastError();
+        return call_error(GUARD_ERR_CUDA, "cudaMemsetAsync: %s", cudaGetErrorString(e));
+    }
+    XentArgs a{};
+    a.x = d_x;
+    a.w = d_w;
+    a.rows = rows;
+    a.width = width;
+    a.vocab = vocab;
+    a.x_stride = x_stride;
+    a.w_stride = w_stride;
+    a.dtype = dtype;
+    a.targets = d_targets;
+    a.target_bits = target_bits;
+    a.ignore = ignore_index;
+    a.lse = d_lse;
+    a.grad_loss = d_grad_loss;
+    a.grad_stride = grad_stride;
+    a.dx = d_dx;
+    a.dw = d_dw;
+    a.workspace = d_workspace;
+    a.status = d_status;
+    if (!d_lse || !d_grad_loss || !on(d_lse, 4) || !on(d_grad_loss, 4)) return call_error(GUARD_ERR_ARG, "d_lse and d_grad_loss must be non-NULL and aligned to their elements");
+    const int rc = xent_check(a, guard_linear_xent_workspace_bytes(rows, width, vocab, 1), workspace_bytes, d_dx, (size_t)rows * width * 2, d_dw, (size_t)vocab * width * 2);
+    if (rc != GUARD_OK) return rc;
+    return launched(launch_xent_grad(a, (cudaStream_t)stream), "cross entropy gradient");
+}
+
 int64_t guard_adamw_blocks(const guard_adamw_tensor *tensors, int n) {
     if (n < 0 || (n > 0 && !tensors)) return -1;
     int64_t blocks = 0;

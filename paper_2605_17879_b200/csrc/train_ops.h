@@ -111,4 +111,22 @@ struct EmbedGradArgs {
 size_t embed_grad_workspace(int64_t n, int64_t rows, int64_t width);
 cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st);
 
+struct XentArgs {
+    const void *x, *w;
+    int64_t rows, width, vocab, x_stride, w_stride;
+    int dtype;               // 1 bfloat16, 2 float16
+    const void *targets;
+    int target_bits;
+    int64_t ignore;
+    float *loss, *lse_out;   // forward
+    const float *lse, *grad_loss;   // backward
+    int64_t grad_stride;     // 0 or 1
+    void *dx, *dw;           // or NULL
+    void *workspace;
+    uint32_t *status;
+};
+size_t xent_workspace(int64_t rows, int64_t width, int64_t vocab, bool grads);
+cudaError_t launch_xent(const XentArgs &x, cudaStream_t st);
+cudaError_t launch_xent_grad(const XentArgs &x, cudaStream_t st);
+
 }  // namespace guard

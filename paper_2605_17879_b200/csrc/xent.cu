@@ -1,0 +1,869 @@
+// Softmax cross entropy of a vocabulary product, and its gradients, without keeping the logits.
+//
+//   z = x w^T;  lse_n = log sum_v exp z_nv;  loss_n = lse_n - z_n,target(n)
+//   G_nv = g_n (exp(z_nv - lse_n) - [v = target(n)]);  dx = G w;  dw = G^T x
+//
+// All four products run on the tensor cores in one kernel frame (product_kernel): a warp loads tiles by TMA, one thread issues
+// tcgen05.mma into TMEM, eight warps read the finished accumulator while the next one is filled.  What differs is the last
+// step on an accumulator: the logits' largest value and sum of exponentials per row (the forward pass), G in 16 bits (the
+// backward pass computes the logits again, a piece of the vocabulary at a time), or a gradient.
+//
+// Bound: the tensor cores, 2 N V D operations per product, but for few rows, where reading w once is what takes the time.
+//
+// Rounding: G is held in the inputs' type, since the tensor cores take both operands in one type; each value is off by at
+// most half a step (relative), as independent of its neighbours as the outputs' own rounding.  In float16 it is scaled by a
+// power of two that brings the largest |g_n| to [2^14, 2^15): exp(z - lse) below 2^-28 of that is lost, and the subnormal
+// range otherwise would be.  Sums are float32.
+//
+// Rows that are ignored take no part: where there are any, the others are gathered first, and whatever the ignored ones
+// hold (NaN among it) reaches nothing.
+#include <cudaTypedefs.h>
+
+#include <type_traits>
+
+#include "tcgen05.cuh"
+#include "train_ops.h"
+
+namespace guard {
+
+namespace {
+
+constexpr int kM = 128, kN = 256, kK = 64;    // a tile: rows, columns, depth of a stage
+constexpr int kStages = 4;
+constexpr int kABytes = kM * kK * 2, kBBytes = kN * kK * 2;
+constexpr int kEpilogueWarps = 8;
+constexpr int kProductThreads = 32 * (4 + kEpilogueWarps);
+constexpr int kProductSmem = kStages * (kABytes + kBBytes) + 1024;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kPart = kN / 2;                 // columns behind one partial result of a row: half a tile
+
+enum Mode { kStats, kGrad, kDx, kDw };
+
+struct Header {         // at the start of the workspace, written by xent_rows_kernel
+    int32_t count;      // rows that take part
+    int32_t whole;      // they are all rows: x is read where it is
+    float scale, inverse;   // of G, and what a gradient is multiplied by
+};
+
+struct ProductArgs {
+    const Header *head;    // or NULL: all rows
+    int rows;              // N
+    int64_t vocab;
+    int m_tiles, n_tiles, k_blocks;   // of the whole problem (the rows' part: at most)
+    int splits;            // of the depth (kDx)
+    int group;             // row tiles that share column tiles while those are in the second-level cache
+    int64_t v0;            // first vocabulary entry of the piece
+    const int32_t *target; // [rows] vocabulary index or -1, by (gathered) row
+    const void *raw_target;   // without a header: int32 or int64 as the caller gave them
+    int target_bits;
+    const float *lse, *grad;  // [rows], by gathered row: log sums and scaled row gradients
+    float2 *parts;         // [rows][n_parts] largest value and sum
+    int n_parts;
+    float *picked;         // [rows] logit of the target
+    void *out;             // G, dx or dw
+    int64_t out_stride;
+    const int32_t *row_of; // gathered row -> row (dx)
+    float *partial;        // [splits][rows padded][width] (kDx)
+    int64_t partial_stride;
+    int add;               // add to partial
+    int64_t width;
+    uint32_t *status;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// What exponents are taken relative to: the largest value, or 0 where that is infinite.
+__device__ __forceinline__ float finite_or_zero(float m) { return fabsf(m) == INFINITY ? 0.0f : m; }
+
+struct alignas(8) ProductShared {
+    uint64_t full[kStages], empty[kStages], done[2], free_[2], drain;
+    uint32_t tmem;
+    uint32_t abort;
+};
+
+// Bounded wait; false when the time ran out here or in another warp.
+__device__ __forceinline__ bool wait_for(ProductShared &s, uint64_t *bar, uint32_t parity) {
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity)) {
+        if (*(volatile uint32_t *)&s.abort) return false;
+        if (clock64() - t0 > kWaitLimitCycles) {
+            *(volatile uint32_t *)&s.abort = 1;
+            return false;
+        }
+    }
+    return true;
+}
+
+struct Tile { int m, n, split; };
+
+// The t-th tile: groups of row tiles, column tile after column tile within a group.
+__device__ __forceinline__ Tile tile_at(int t, int m_tiles, int n_tiles, int group, int splits) {
+    Tile r;
+    r.split = t % splits;
+    t /= splits;
+    const int per = group * n_tiles;
+    const int g = t / per, first = g * group;
+    const int high = min(group, m_tiles - first);
+    const int in = t - g * per;
+    r.m = first + in % high;
+    r.n = in / high;
+    return r;
+}
+
+template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// 32 values of a row to 16-bit memory, those before `left`.
+template <typename T>
+__device__ __forceinline__ void store_row32(T *p, int left, bool wide, const float (&x)[32]) {
+    if (wide && left >= 32) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            uint4 w;
+            w.x = pack2<T>(x[8 * q], x[8 * q + 1]);
+            w.y = pack2<T>(x[8 * q + 2], x[8 * q + 3]);
+            w.z = pack2<T>(x[8 * q + 4], x[8 * q + 5]);
+            w.w = pack2<T>(x[8 * q + 6], x[8 * q + 7]);
+            reinterpret_cast<uint4 *>(p)[q] = w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (j < left) p[j] = Conv<T>::down(x[j]);
+}
+
+template <int MODE, typename T>
+__global__ void __launch_bounds__(kProductThreads, 1)
+product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a2, const __grid_constant__ CUtensorMap map_b,
+               const __grid_constant__ CUtensorMap map_b2, const ProductArgs a) {
+    extern __shared__ uint8_t raw[];
+    __shared__ ProductShared s;
+    uint8_t *tiles = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+    const int warp = warp_id(), lane = lane_id();
+    pdl_wait();
+
+    const int rows = a.head ? a.head->count : a.rows;
+    const bool whole = a.head ? a.head->whole != 0 : true;
+    int m_tiles = a.m_tiles, k_blocks = a.k_blocks;
+    if (MODE == kDw) k_blocks = (rows + kK - 1) / kK;
+    else m_tiles = (rows + kM - 1) / kM;
+    const int total = m_tiles * a.n_tiles * a.splits;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&s.full[i], 1);
+            mbar_init(&s.empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s.done[i], 1);
+            mbar_init(&s.free_[i], kEpilogueWarps);
+        }
+        mbar_init(&s.drain, 1);
+        s.abort = 0;
+    }
+    if (warp == 2) tmem_alloc(&s.tmem, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s.tmem;
+
+    if (warp == 0 && lane == 0) {
+        // ---- loads
+        // the rows' operand: x, which is read where it is when every row takes part (A of the logits, B of dw)
+        const CUtensorMap *pa = MODE == kStats || MODE == kGrad ? (whole ? &map_a : &map_a2) : &map_a;
+        const CUtensorMap *pb = MODE == kDw ? (whole ? &map_b : &map_b2) : &map_b;
+        tma_prefetch_map(pa);
+        tma_prefetch_map(pb);
+        uint32_t it = 0;
+        bool ok = true;
+        for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
+            const Tile tl = tile_at(t, m_tiles, a.n_tiles, a.group, a.splits);
+            const int k0 = (int)((int64_t)k_blocks * tl.split / a.splits), k1 = (int)((int64_t)k_blocks * (tl.split + 1) / a.splits);
+            for (int k = k0; k < k1; ++k, ++it) {
+                const int st = it % kStages;
+                if (!(ok = wait_for(s, &s.empty[st], ((it / kStages) & 1) ^ 1))) break;
+                uint8_t *sa = tiles + st * (kABytes + kBBytes), *sb = sa + kABytes;
+                mbar_arrive_expect_tx(&s.full[st], kABytes + kBBytes);
+                if (MODE == kDw) {          // A: G, tokens by vocabulary; the vocabulary (rows of dw) is contiguous
+                    for (int h = 0; h < kM / 64; ++h) tma_load(sa + h * 8192, pa, tl.m * kM + h * 64, k * kK, &s.full[st]);
+                } else {
+                    tma_load(sa, pa, k * kK, tl.m * kM, &s.full[st]);
+                }
+                if (MODE == kStats || MODE == kGrad) {
+                    tma_load(sb, pb, k * kK, (int)a.v0 + tl.n * kN, &s.full[st]);
+                } else {                    // B: w or x, whose columns (of the result) are contiguous
+                    const int y = MODE == kDx ? (int)a.v0 + k * kK : k * kK;
+                    for (int h = 0; h < kN / 64; ++h) tma_load(sb + h * 8192, pb, tl.n * kN + h * 64, y, &s.full[st]);
+                }
+            }
+        }
+        if (*(volatile uint32_t *)&s.abort) {       // given up: let the copies in flight land before the memory is anyone else's
+            for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) {
+                const long long t0 = clock64();
+                while (!mbar_try_wait(&s.full[i % kStages], (i / kStages) & 1) && clock64() - t0 < kWaitLimitCycles) {}
+            }
+        }
+    } else if (warp == 1 && lane == 0) {
+        // ---- products
+        constexpr uint32_t type = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+        constexpr uint32_t a_rows_contiguous = MODE == kDw, b_rows_contiguous = MODE == kDx || MODE == kDw;
+        constexpr uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | (a_rows_contiguous << 15) | (b_rows_contiguous << 16) |
+                                   ((kN / 8) << 17) | ((kM / 16) << 24);
+        uint32_t it = 0, nth = 0;
+        bool ok = true;
+        for (int t = blockIdx.x; t < total && ok; t += gridDim.x, ++nth) {
+            const int split = t % a.splits;
+            const int k0 = (int)((int64_t)k_blocks * split / a.splits), k1 = (int)((int64_t)k_blocks * (split + 1) / a.splits);
+            const uint32_t acc = nth & 1;
+            if (!(ok = wait_for(s, &s.free_[acc], ((nth >> 1) & 1) ^ 1))) break;
+            tc_fence_after();
+            for (int k = k0; k < k1; ++k, ++it) {
+                const int st = it % kStages;
+                if (!(ok = wait_for(s, &s.full[st], (it / kStages) & 1))) break;
+                tc_fence_after();
+                const uint8_t *sa = tiles + st * (kABytes + kBBytes), *sb = sa + kABytes;
+#pragma unroll
+                for (int j = 0; j < kK / 16; ++j) {
+                    // depth contiguous: 16 elements on in a row of 128 bytes; rows contiguous: 16 rows of 128 bytes on
+                    const uint64_t da = smem_desc(sa + (a_rows_contiguous ? j * 2048 : j * 32), 8192, 1024);
+                    const uint64_t db = smem_desc(sb + (b_rows_contiguous ? j * 2048 : j * 32), 8192, 1024);
+                    tc_mma(tmem + acc * kN, da, db, idesc, k > k0 || j > 0);
+                }
+                tc_commit(&s.empty[st]);
+            }
+            if (ok) tc_commit(&s.done[acc]);
+        }
+        if (*(volatile uint32_t *)&s.abort) {
+            tc_commit(&s.drain);
+            const long long t0 = clock64();
+            while (!mbar_try_wait(&s.drain, 0) && clock64() - t0 < kWaitLimitCycles) {}
+        }
+    } else if (warp >= 4) {
+        // ---- what becomes of an accumulator: a thread has a row, and half of its columns
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const float inverse = a.head ? a.head->inverse : 1.0f;
+        uint32_t nth = 0;
+        for (int t = blockIdx.x; t < total; t += gridDim.x, ++nth) {
+            const Tile tl = tile_at(t, m_tiles, a.n_tiles, a.group, a.splits);
+            const uint32_t acc = nth & 1;
+            const int row = tl.m * kM + quarter * 32 + lane;
+            bool empty = false;       // no depth at all: the accumulator was not written
+            if (MODE == kDw || MODE == kDx)
+                empty = (int)((int64_t)k_blocks * tl.split / a.splits) == (int)((int64_t)k_blocks * (tl.split + 1) / a.splits);
+            int64_t target = -1;
+            float lse2 = 0.0f, g = 0.0f;
+            if (MODE == kStats || MODE == kGrad) {
+                if (row < rows) {
+                    if (a.target) target = a.target[row];
+                    else target = a.target_bits == 64 ? reinterpret_cast<const long long *>(a.raw_target)[row] : reinterpret_cast<const int *>(a.raw_target)[row];
+                    if (MODE == kGrad) {
+                        lse2 = __fmul_rn(a.lse[row], kLog2e);
+                        g = a.grad[row];
+                    }
+                }
+            }
+            if (!__all_sync(0xFFFFFFFFu, wait_for(s, &s.done[acc], (nth >> 1) & 1))) break;   // (the warp stays together)
+            tc_fence_after();
+            float top = -INFINITY, sum = 0.0f;
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                uint32_t r[32];
+                float x[32];
+                tmem_load32(tmem + lanes + acc * kN + half * 128 + c * 32, r);
+                tmem_load_wait();
+                if (c == 3) {         // the accumulator is free once every warp has read its part
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&s.free_[acc]);
+                }
+                const int64_t col = (int64_t)tl.n * kN + half * 128 + c * 32;
+                if (MODE == kStats || MODE == kGrad) {
+                    const int64_t first = a.v0 + col;
+                    const int64_t at = target - first;
+                    const bool here = at >= 0 && at < 32;
+                    const int left = (int)min((int64_t)32, max((int64_t)0, a.vocab - first));
+                    if (MODE == kStats) {
+                        if (left < 32) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (j >= left) r[j] = 0xFF800000u;
+                        }
+                        if (__any_sync(0xFFFFFFFFu, here)) {
+                            float z = 0.0f;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (j == (int)at) z = __uint_as_float(r[j]);
+                            if (here) a.picked[row] = z;
+                        }
+                        float most = top;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) most = fmaxf(most, __uint_as_float(r[j]));
+                        const float base = finite_or_zero(most);
+                        const float shift = -__fmul_rn(base, kLog2e);
+                        if (sum != 0.0f) sum = __fmul_rn(sum, exp2_fast(__fmul_rn(__fsub_rn(finite_or_zero(top), base), kLog2e)));
+                        float part[4] = {};
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) part[j & 3] = __fadd_rn(part[j & 3], exp2_fast(__fmaf_rn(__uint_as_float(r[j]), kLog2e, shift)));
+                        sum = __fadd_rn(sum, __fadd_rn(__fadd_rn(part[0], part[1]), __fadd_rn(part[2], part[3])));
+                        top = most;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            float p = exp2_fast(__fmaf_rn(__uint_as_float(r[j]), kLog2e, -lse2));
+                            if (j == (int)at && here) p = __fsub_rn(p, 1.0f);
+                            x[j] = j < left && row < rows ? __fmul_rn(p, g) : 0.0f;
+                        }
+                        // (G has whole tiles: its padding is written as zeros)
+                        store_row32(reinterpret_cast<T *>(a.out) + (int64_t)row * a.out_stride + col, 32, true, x);
+                    }
+                } else {
+                    const int left = (int)min((int64_t)32, max((int64_t)0, a.width - col));
+                    if (MODE == kDx && a.partial) {
+                        float *p = a.partial + tl.split * a.partial_stride + (int64_t)row * a.width + col;
+                        if (row < rows) {
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+                                if (4 * q < left) {        // (the width is a multiple of eight)
+                                    float4 y = make_float4(__uint_as_float(r[4 * q]), __uint_as_float(r[4 * q + 1]), __uint_as_float(r[4 * q + 2]),
+                                                           __uint_as_float(r[4 * q + 3]));
+                                    if (empty) y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                                    if (a.add) {
+                                        const float4 z = reinterpret_cast<const float4 *>(p)[q];
+                                        y = make_float4(__fadd_rn(z.x, y.x), __fadd_rn(z.y, y.y), __fadd_rn(z.z, y.z), __fadd_rn(z.w, y.w));
+                                    }
+                                    reinterpret_cast<float4 *>(p)[q] = y;
+                                }
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) x[j] = empty ? 0.0f : __fmul_rn(__uint_as_float(r[j]), inverse);
+                        const int64_t most = MODE == kDx ? rows : a.vocab - a.v0;     // rows of the result
+                        if (row < most) {
+                            const int64_t to = MODE == kDx ? (a.row_of && !whole ? a.row_of[row] : row) : a.v0 + row;
+                            store_row32(reinterpret_cast<T *>(a.out) + to * a.out_stride + col, left, true, x);
+                        }
+                    }
+                }
+            }
+            if (MODE == kStats && row < rows) a.parts[(int64_t)row * a.n_parts + tl.n * 2 + half] = make_float2(top, sum);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (threadIdx.x == 0 && s.abort && a.status) atomicOr(a.status, kStatTimeout);
+    if (warp == 2) tmem_free(tmem, 512);
+}
+
+// ---- rows that take part ----------------------------------------------------------------------------------------------
+
+struct RowsArgs {
+    const void *targets;
+    int bits;
+    int rows, padded;
+    int64_t vocab, ignore;
+    Header *head;
+    int32_t *target;       // [padded] by gathered row
+    int32_t *row_of;       // [padded] gathered row -> row
+    int32_t *place;        // [rows] row -> gathered row, or -1
+    const float *lse, *grad;   // backward: by row
+    int64_t grad_stride;       // 0: one value for all rows
+    float *lse_to, *grad_to;   // by gathered row
+    bool half;             // scale the row gradients for float16
+    float *loss, *lse_out; // forward: by row, written for those that take no part
+    uint32_t *status;
+};
+
+__device__ __forceinline__ int64_t target_at(const void *t, int bits, int64_t i) {
+    return bits == 64 ? reinterpret_cast<const long long *>(t)[i] : (int64_t) reinterpret_cast<const int *>(t)[i];
+}
+
+// One CTA walks over the rows in order.
+__global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a) {
+    __shared__ int s_count[32];
+    __shared__ float s_top[32];
+    pdl_wait();
+    const int lane = lane_id(), warp = warp_id();
+    float scale = 1.0f, inverse = 1.0f;
+    if (a.half) {                      // a power of two that brings the largest |g| to [2^14, 2^15)
+        float top = 0.0f;
+        for (int i = threadIdx.x; i < a.rows; i += 1024) {
+            const int64_t t = target_at(a.targets, a.bits, i);
+            if (t != a.ignore && t >= 0 && t < a.vocab) top = fmaxf(top, fabsf(a.grad[i * a.grad_stride]));
+        }
+        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        if (lane == 0) s_top[warp] = top;
+        __syncthreads();
+        for (int w = 0; w < 32; ++w) top = fmaxf(top, s_top[w]);
+        if (top > 0.0f && top < INFINITY) {
+            int e;
+            frexpf(top, &e);           // top in [2^(e-1), 2^e)
+            e = min(max(15 - e, -120), 120);
+            scale = ldexpf(1.0f, e);
+            inverse = ldexpf(1.0f, -e);
+        }
+    }
+    int before = 0;
+    for (int64_t base = 0; base < a.rows; base += 1024) {
+        const int64_t i = base + threadIdx.x;
+        bool in = false;
+        int64_t t = -1;
+        if (i < a.rows) {
+            t = target_at(a.targets, a.bits, i);
+            const bool bad = t != a.ignore && (t < 0 || t >= a.vocab);
+            in = t != a.ignore && !bad;
+            if (bad && a.status) atomicOr(a.status, kStatIndex);
+            if (!in && a.loss) {
+                a.loss[i] = bad ? __uint_as_float(0x7FC00000u) : 0.0f;
+                a.lse_out[i] = 0.0f;
+            }
+        }
+        const uint32_t votes = __ballot_sync(0xFFFFFFFFu, in);
+        if (lane == 0) s_count[warp] = __popc(votes);
+        __syncthreads();
+        int at = before, all = 0;
+        for (int w = 0; w < 32; ++w) {
+            if (w < warp) at += s_count[w];
+            all += s_count[w];
+        }
+        at += __popc(votes & ((1u << lane) - 1));
+        if (in) {
+            a.target[at] = (int32_t)t;
+            a.row_of[at] = (int32_t)i;
+            if (a.lse_to) {
+                a.lse_to[at] = a.lse[i];
+                a.grad_to[at] = __fmul_rn(a.grad[i * a.grad_stride], scale);
+            }
+        }
+        if (i < a.rows) a.place[i] = in ? at : -1;
+        before += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        a.head->count = before;
+        a.head->whole = before == a.rows;
+        a.head->scale = scale;
+        a.head->inverse = inverse;
+    }
+}
+
+struct GatherArgs {
+    const Header *head;
+    const int32_t *place;
+    int rows, padded;
+    const void *x;
+    int64_t stride;
+    int vectors;           // 16-byte vectors of a row
+    void *to;              // [padded][vectors]
+    void *dx;              // or NULL: rows that take no part become zero
+};
+
+// Gathers the rows that take part, with zeros up to a whole tile; a warp per row.
+__global__ void __launch_bounds__(256) xent_gather_kernel(const GatherArgs a) {
+    pdl_wait();
+    if (a.head->whole) return;
+    const int count = a.head->count;
+    const int padded = (count + kM - 1) / kM * kM;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    for (int64_t r = (int64_t)blockIdx.x * 8 + warp_id(); r < a.rows + kM; r += (int64_t)gridDim.x * 8) {
+        if (r >= a.rows) {             // padding rows
+            const int64_t p = count + (r - a.rows);
+            if (p < padded)
+                for (int v = lane_id(); v < a.vectors; v += 32) reinterpret_cast<uint4 *>(a.to)[p * a.vectors + v] = zero;
+            continue;
+        }
+        const int at = a.place[r];
+        if (at >= 0) {
+            const uint4 *from = reinterpret_cast<const uint4 *>((const char *)a.x + r * a.stride * 2);
+            for (int v = lane_id(); v < a.vectors; v += 32) reinterpret_cast<uint4 *>(a.to)[(int64_t)at * a.vectors + v] = from[v];
+        } else if (a.dx) {
+            for (int v = lane_id(); v < a.vectors; v += 32) reinterpret_cast<uint4 *>(a.dx)[r * a.vectors + v] = zero;
+        }
+    }
+}
+
+struct CombineArgs {
+    const Header *head;    // or NULL: all rows, targets as the caller gave them
+    int rows;
+    const void *targets;
+    int bits;
+    int64_t vocab, ignore;
+    const int32_t *row_of;
+    const float2 *parts;
+    int n_parts;
+    const float *picked;
+    float *loss, *lse;
+    uint32_t *status;
+};
+
+// A warp per row joins its partial results.
+__global__ void __launch_bounds__(256) xent_combine_kernel(const CombineArgs a) {
+    pdl_wait();
+    const int rows = a.head ? a.head->count : a.rows;
+    for (int64_t r = (int64_t)blockIdx.x * 8 + warp_id(); r < rows; r += (int64_t)gridDim.x * 8) {
+        const int64_t to = a.head ? a.row_of[r] : r;
+        if (!a.head) {
+            const int64_t t = target_at(a.targets, a.bits, r);
+            const bool bad = t != a.ignore && (t < 0 || t >= a.vocab);
+            if (t == a.ignore || bad) {
+                if (lane_id() == 0) {
+                    if (bad && a.status) atomicOr(a.status, kStatIndex);
+                    a.loss[to] = bad ? __uint_as_float(0x7FC00000u) : 0.0f;
+                    a.lse[to] = 0.0f;
+                }
+                continue;
+            }
+        }
+        const float2 *p = a.parts + r * a.n_parts;
+        float top = -INFINITY, sum = 0.0f;
+        for (int i = lane_id(); i < a.n_parts; i += 32) {
+            const float2 q = p[i];
+            const float most = fmaxf(top, q.x), base = finite_or_zero(most);
+            // (nothing summed yet, or an empty part: its exponent says nothing)
+            const float x = sum != 0.0f ? __fmul_rn(sum, exp2_fast(__fmul_rn(__fsub_rn(finite_or_zero(top), base), kLog2e))) : 0.0f;
+            const float y = q.y != 0.0f ? __fmul_rn(q.y, exp2_fast(__fmul_rn(__fsub_rn(finite_or_zero(q.x), base), kLog2e))) : 0.0f;
+            sum = __fadd_rn(x, y);
+            top = most;
+        }
+        for (int d = 16; d > 0; d >>= 1) {
+            const float t2 = __shfl_xor_sync(0xFFFFFFFFu, top, d), s2 = __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+            const float most = fmaxf(top, t2), base = finite_or_zero(most);
+            const float x = sum != 0.0f ? __fmul_rn(sum, exp2_fast(__fmul_rn(__fsub_rn(finite_or_zero(top), base), kLog2e))) : 0.0f;
+            const float y = s2 != 0.0f ? __fmul_rn(s2, exp2_fast(__fmul_rn(__fsub_rn(finite_or_zero(t2), base), kLog2e))) : 0.0f;
+            sum = __fadd_rn(x, y);
+            top = most;
+        }
+        if (lane_id() == 0) {
+            const float lse = __fadd_rn(finite_or_zero(top), logf(sum));
+            a.loss[to] = __fsub_rn(lse, a.picked[r]);
+            a.lse[to] = lse;
+        }
+    }
+}
+
+struct JoinArgs {
+    const Header *head;
+    const int32_t *row_of;
+    int64_t rows, width;
+    const float *partial;
+    int64_t stride;
+    int splits;
+    void *dx;
+};
+
+// dx from its partial sums, in order.
+template <typename T>
+__global__ void __launch_bounds__(256) xent_join_kernel(const JoinArgs a) {
+    pdl_wait();
+    const int64_t groups = a.width / 8, work = a.head->count * groups;
+    const float inverse = a.head->inverse;
+    const bool whole = a.head->whole != 0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < work; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / groups, col = (i - r * groups) * 8;
+        float x[8] = {};
+        for (int k = 0; k < a.splits; ++k) {
+            const float4 *p = reinterpret_cast<const float4 *>(a.partial + k * a.stride + r * a.width + col);
+            const float4 u = p[0], v = p[1];
+            const float y[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = __fadd_rn(x[j], y[j]);
+        }
+        uint4 w;
+        w.x = pack2<T>(__fmul_rn(x[0], inverse), __fmul_rn(x[1], inverse));
+        w.y = pack2<T>(__fmul_rn(x[2], inverse), __fmul_rn(x[3], inverse));
+        w.z = pack2<T>(__fmul_rn(x[4], inverse), __fmul_rn(x[5], inverse));
+        w.w = pack2<T>(__fmul_rn(x[6], inverse), __fmul_rn(x[7], inverse));
+        *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(a.dx) + (whole ? r : a.row_of[r]) * a.width + col) = w;
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+PFN_cuTensorMapEncodeTiled encoder() {
+    static PFN_cuTensorMapEncodeTiled fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            p = nullptr;
+        }
+        return (PFN_cuTensorMapEncodeTiled)p;
+    }();
+    return fn;
+}
+
+// A row-major matrix of 16-bit elements in boxes of 64 columns (128 bytes, swizzled) by `box` rows; outside it reads zeros.
+bool make_map(CUtensorMap *map, bool bf16, const void *p, int64_t width, int64_t rows, int64_t stride, int box) {
+    const PFN_cuTensorMapEncodeTiled encode = encoder();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)(rows < 1 ? 1 : rows)};
+    const cuuint64_t strides[1] = {(cuuint64_t)stride * 2};
+    const cuuint32_t boxes[2] = {64, (cuuint32_t)box};
+    const cuuint32_t steps[2] = {1, 1};
+    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(p), dims, strides, boxes, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int kDirectRows = kM;       // up to here the forward pass takes the rows as they are: there is no tile to save
+
+struct XentLayout {
+    size_t head, target, row_of, place, lse, grad, picked, parts, x, g, partial, total;
+    int64_t padded, piece, partial_stride;
+    int n_parts, splits;
+};
+
+// What a row tile's share of the second-level cache allows the G of one piece to take.
+constexpr int64_t kPieceBytes = 512ll << 20;
+
+XentLayout layout(int64_t rows, int64_t width, int64_t vocab, bool grads) {
+    XentLayout L{};
+    L.padded = (rows + kM - 1) / kM * kM;
+    const int64_t n_tiles = (vocab + kN - 1) / kN;
+    size_t off = 0;
+    auto take = [&](size_t &at, size_t bytes) { at = off, off = up256(off + bytes); };
+    take(L.head, sizeof(Header));
+    take(L.target, L.padded * 4);
+    take(L.row_of, L.padded * 4);
+    take(L.place, rows * 4);
+    take(L.x, grads || rows > kDirectRows ? L.padded * width * 2 : 0);
+    if (!grads) {
+        L.n_parts = (int)(n_tiles * 2);
+        take(L.picked, L.padded * 4);
+        take(L.parts, (size_t)L.padded * L.n_parts * sizeof(float2));
+    } else {
+        take(L.lse, L.padded * 4);
+        take(L.grad, L.padded * 4);
+        int64_t piece = kPieceBytes / (L.padded * 2) / kN * kN;
+        if (piece < kN) piece = kN;
+        const int64_t pieces = (n_tiles * kN + piece - 1) / piece;
+        piece = ((n_tiles + pieces - 1) / pieces) * kN;
+        L.piece = piece;
+        take(L.g, (size_t)L.padded * piece * 2);
+        const int64_t tiles = L.padded / kM * ((width + kN - 1) / kN);
+        int64_t splits = sm_count() / tiles;
+        const int64_t depth = piece / kK;
+        if (splits > depth / 4) splits = depth / 4;
+        if (splits < 1) splits = 1;
+        L.splits = (int)splits;
+        L.partial_stride = L.padded * width;
+        take(L.partial, splits > 1 || pieces > 1 ? (size_t)splits * L.partial_stride * 4 : 0);
+    }
+    L.total = off;
+    return L;
+}
+
+template <int MODE, typename T>
+cudaError_t launch_product(const CUtensorMap &ma, const CUtensorMap &ma2, const CUtensorMap &mb, const CUtensorMap &mb2, const ProductArgs &a, cudaStream_t st) {
+    cudaError_t e = cudaFuncSetAttribute(product_kernel<MODE, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
+    if (e != cudaSuccess) return e;
+    const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * a.splits;
+    const int64_t sms = sm_count();
+    return launch_after_smem(product_kernel<MODE, T>, dim3((unsigned)(tiles < sms ? tiles : sms)), dim3(kProductThreads), kProductSmem, st, ma, ma2, mb, mb2, a);
+}
+
+// Row tiles that share a column tile: as many as fit in about a third of the second-level cache.
+int group_of(int64_t depth_bytes, int m_tiles) {
+    int64_t g = (40ll << 20) / (depth_bytes * kM);
+    if (g < 8) g = 8;
+    return (int)(g < m_tiles ? g : m_tiles);
+}
+
+cudaError_t launch_rows(const XentArgs &x, const XentLayout &L, bool grads, cudaStream_t st) {
+    char *ws = (char *)x.workspace;
+    RowsArgs r{};
+    r.targets = x.targets;
+    r.bits = x.target_bits;
+    r.rows = (int)x.rows;
+    r.padded = (int)L.padded;
+    r.vocab = x.vocab;
+    r.ignore = x.ignore;
+    r.head = (Header *)(ws + L.head);
+    r.target = (int32_t *)(ws + L.target);
+    r.row_of = (int32_t *)(ws + L.row_of);
+    r.place = (int32_t *)(ws + L.place);
+    r.status = x.status;
+    if (grads) {
+        r.lse = x.lse;
+        r.grad = x.grad_loss;
+        r.grad_stride = x.grad_stride;
+        r.lse_to = (float *)(ws + L.lse);
+        r.grad_to = (float *)(ws + L.grad);
+        r.half = x.dtype == 2;
+    } else {
+        r.loss = x.loss;
+        r.lse_out = x.lse_out;
+    }
+    cudaError_t e = launch_after(xent_rows_kernel, dim3(1), dim3(1024), st, r);
+    if (e != cudaSuccess) return e;
+    GatherArgs g{};
+    g.head = r.head;
+    g.place = r.place;
+    g.rows = r.rows;
+    g.padded = r.padded;
+    g.x = x.x;
+    g.stride = x.x_stride;
+    g.vectors = (int)(x.width / 8);
+    g.to = ws + L.x;
+    g.dx = grads ? x.dx : nullptr;
+    int64_t grid = (x.rows + kM + 7) / 8;
+    if (grid > sm_count() * 8) grid = sm_count() * 8;
+    return launch_after(xent_gather_kernel, dim3((unsigned)grid), dim3(256), st, g);
+}
+
+template <typename T>
+cudaError_t forward(const XentArgs &x, cudaStream_t st) {
+    const XentLayout L = layout(x.rows, x.width, x.vocab, false);
+    char *ws = (char *)x.workspace;
+    const bool direct = x.rows <= kDirectRows, bf16 = x.dtype == 1;
+    cudaError_t e;
+    CUtensorMap mx, mg, mw;
+    if (!make_map(&mx, bf16, x.x, x.width, x.rows, x.x_stride, kM) || !make_map(&mw, bf16, x.w, x.width, x.vocab, x.w_stride, kN)) return cudaErrorInvalidValue;
+    mg = mx;
+    if (!direct) {
+        if (!make_map(&mg, bf16, ws + L.x, x.width, L.padded, x.width, kM)) return cudaErrorInvalidValue;
+        e = launch_rows(x, L, false, st);
+        if (e != cudaSuccess) return e;
+    }
+    ProductArgs a{};
+    a.head = direct ? nullptr : (const Header *)(ws + L.head);
+    a.rows = (int)x.rows;
+    a.vocab = x.vocab;
+    a.width = x.width;
+    a.m_tiles = (int)(L.padded / kM);
+    a.n_tiles = (int)((x.vocab + kN - 1) / kN);
+    a.k_blocks = (int)((x.width + kK - 1) / kK);
+    a.splits = 1;
+    a.group = group_of(x.width * 2, a.m_tiles);
+    a.target = direct ? nullptr : (const int32_t *)(ws + L.target);
+    a.raw_target = x.targets;
+    a.target_bits = x.target_bits;
+    a.parts = (float2 *)(ws + L.parts);
+    a.n_parts = L.n_parts;
+    a.picked = (float *)(ws + L.picked);
+    a.status = x.status;
+    e = launch_product<kStats, T>(mx, mg, mw, mw, a, st);
+    if (e != cudaSuccess) return e;
+    CombineArgs c{};
+    c.head = a.head;
+    c.rows = (int)x.rows;
+    c.targets = x.targets;
+    c.bits = x.target_bits;
+    c.vocab = x.vocab;
+    c.ignore = x.ignore;
+    c.row_of = (const int32_t *)(ws + L.row_of);
+    c.parts = a.parts;
+    c.n_parts = a.n_parts;
+    c.picked = a.picked;
+    c.loss = x.loss;
+    c.lse = x.lse_out;
+    c.status = x.status;
+    int64_t grid = (x.rows + 7) / 8;
+    if (grid > sm_count() * 8) grid = sm_count() * 8;
+    return launch_after(xent_combine_kernel, dim3((unsigned)grid), dim3(256), st, c);
+}
+
+template <typename T>
+cudaError_t backward(const XentArgs &x, cudaStream_t st) {
+    const XentLayout L = layout(x.rows, x.width, x.vocab, true);
+    char *ws = (char *)x.workspace;
+    const bool bf16 = x.dtype == 1;
+    cudaError_t e = launch_rows(x, L, true, st);
+    if (e != cudaSuccess) return e;
+    CUtensorMap mx, mxg, mw, gk, gm, wn, xn, xng;
+    // G as the rows' operand of dx (its vocabulary is the depth) and of dw (its vocabulary are the rows)
+    if (!make_map(&mx, bf16, x.x, x.width, x.rows, x.x_stride, kM) || !make_map(&mxg, bf16, ws + L.x, x.width, L.padded, x.width, kM) ||
+        !make_map(&mw, bf16, x.w, x.width, x.vocab, x.w_stride, kN) || !make_map(&gk, bf16, ws + L.g, L.piece, L.padded, L.piece, kM) ||
+        !make_map(&gm, bf16, ws + L.g, L.piece, L.padded, L.piece, kK) || !make_map(&wn, bf16, x.w, x.width, x.vocab, x.w_stride, kK) ||
+        !make_map(&xn, bf16, x.x, x.width, x.rows, x.x_stride, kK) || !make_map(&xng, bf16, ws + L.x, x.width, L.padded, x.width, kK))
+        return cudaErrorInvalidValue;
+    const int64_t pieces = (x.vocab + L.piece - 1) / L.piece;
+    const bool direct = L.splits == 1 && pieces == 1;
+    ProductArgs a{};
+    a.head = (const Header *)(ws + L.head);
+    a.rows = (int)x.rows;
+    a.vocab = x.vocab;
+    a.width = x.width;
+    a.target = (const int32_t *)(ws + L.target);
+    a.lse = (const float *)(ws + L.lse);
+    a.grad = (const float *)(ws + L.grad);
+    a.row_of = (const int32_t *)(ws + L.row_of);
+    a.status = x.status;
+    const int row_tiles = (int)(L.padded / kM), width_tiles = (int)((x.width + kN - 1) / kN);
+    for (int64_t p = 0; p < pieces; ++p) {
+        a.v0 = p * L.piece;
+        const int64_t here = x.vocab - a.v0 < L.piece ? x.vocab - a.v0 : L.piece;
+        ProductArgs g = a;
+        g.m_tiles = row_tiles;
+        g.n_tiles = (int)((here + kN - 1) / kN);
+        g.k_blocks = (int)((x.width + kK - 1) / kK);
+        g.splits = 1;
+        g.group = group_of(x.width * 2, g.m_tiles);
+        g.out = ws + L.g;
+        g.out_stride = L.piece;
+        e = launch_product<kGrad, T>(mx, mxg, mw, mw, g, st);
+        if (e != cudaSuccess) return e;
+        if (x.dx) {
+            ProductArgs d = a;
+            d.m_tiles = row_tiles;
+            d.n_tiles = width_tiles;
+            d.k_blocks = (int)((here + kK - 1) / kK);
+            d.splits = L.splits;
+            d.group = row_tiles < 16 ? row_tiles : 16;
+            d.out = x.dx;
+            d.out_stride = x.width;
+            d.partial = direct ? nullptr : (float *)(ws + L.partial);
+            d.partial_stride = L.partial_stride;
+            d.add = p > 0;
+            e = launch_product<kDx, T>(gk, gk, wn, wn, d, st);
+            if (e != cudaSuccess) return e;
+        }
+        if (x.dw) {
+            ProductArgs d = a;
+            d.m_tiles = (int)((here + kM - 1) / kM);
+            d.n_tiles = width_tiles;
+            d.splits = 1;
+            d.group = d.m_tiles < 16 ? d.m_tiles : 16;
+            d.out = x.dw;
+            d.out_stride = x.width;
+            e = launch_product<kDw, T>(gm, gm, xn, xng, d, st);
+            if (e != cudaSuccess) return e;
+        }
+    }
+    if (x.dx && !direct) {
+        JoinArgs j{};
+        j.head = a.head;
+        j.row_of = a.row_of;
+        j.rows = x.rows;
+        j.width = x.width;
+        j.partial = (const float *)(ws + L.partial);
+        j.stride = L.partial_stride;
+        j.splits = L.splits;
+        j.dx = x.dx;
+        int64_t grid = (x.rows * (x.width / 8) + 255) / 256;
+        if (grid > sm_count() * 8) grid = sm_count() * 8;
+        return launch_after(xent_join_kernel<T>, dim3((unsigned)grid), dim3(256), st, j);
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+size_t xent_workspace(int64_t rows, int64_t width, int64_t vocab, bool grads) { return layout(rows, width, vocab, grads).total; }
+cudaError_t launch_xent(const XentArgs &x, cudaStream_t st) { return x.dtype == 1 ? forward<__nv_bfloat16>(x, st) : forward<__half>(x, st); }
+cudaError_t launch_xent_grad(const XentArgs &x, cudaStream_t st) { return x.dtype == 1 ? backward<__nv_bfloat16>(x, st) : backward<__half>(x, st); }
+
+}  // namespace guard

@@ -44,6 +44,9 @@ def lib():
                 ("guard_embed", i, [vp, i, i64, vp, i64, i64, i64, i, f, vp, vp, vp]),
                 ("guard_embed_grad_workspace_bytes", z, [i64, i64, i64]),
                 ("guard_embed_grad", i, [vp, i64, i, vp, i, i64, i64, i64, f, i64, i, vp, vp, z, vp, vp]),
+                ("guard_linear_xent_workspace_bytes", z, [i64, i64, i64, i]),
+                ("guard_linear_xent", i, [vp, i64, vp, i64, i64, i64, i64, i, vp, i, i64, vp, vp, vp, z, vp, vp]),
+                ("guard_linear_xent_grad", i, [vp, i64, vp, i64, i64, i64, i64, i, vp, i, i64, vp, vp, i, vp, vp, vp, z, vp, vp]),
                 ("guard_adamw_blocks", i64, [tp, i]),
                 ("guard_adamw_workspace_bytes", z, [tp, i]),
                 ("guard_adamw_create", i, [C.POINTER(vp), tp, i, i, i, i, d, d, d, vp, vp, vp, vp, i64, C.c_uint32, vp, z, vp]),
@@ -187,6 +190,63 @@ def embed_grad(grad: torch.Tensor, tokens: torch.Tensor, rows: int, *, scale: fl
         ws = _workspace(workspace, lib().guard_embed_grad_workspace_bytes(n, rows, width), dev)
         _check(lib().guard_embed_grad(grad.data_ptr(), stride, code, tokens.data_ptr(), bits, n, rows, width, scale, padding_idx,
                                       1 if accumulate else 0, to, ws.data_ptr(), ws.numel(), _status_ptr(out, dev), guard._stream()))
+    return out
+
+
+def _product(x, w, targets):
+    dev = _cuda(x, "x")
+    _cuda(w, "w", dev)
+    bits = _tokens(targets, dev)
+    code = _dtype(x, "x")
+    if w.dtype != x.dtype or code == 0:
+        raise ValueError("x and w must both be bfloat16 or both float16, got %s and %s" % (x.dtype, w.dtype))
+    xs, wst = _rows(x, "x"), _rows(w, "w")
+    if x.shape[1] != w.shape[1] or targets.numel() != x.shape[0]:
+        raise ValueError("need x [rows, width], w [vocab, width] and rows targets")
+    return dev, bits, code, xs, wst
+
+
+def linear_xent(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, *, ignore_index: int = -100,
+                workspace: Optional[torch.Tensor] = None, out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """Softmax cross entropy of the logits x @ w.T against targets, row by row, without keeping the logits: float32
+    out["loss"] and out["lse"] (the logits' log sum of exponentials, which the gradient takes).  x [rows, width] and
+    w [vocab, width]: bfloat16 or float16, width a multiple of 8.  Rows whose target is ignore_index have 0 in both."""
+    dev, bits, code, xs, wst = _product(x, w, targets)
+    rows, width = x.shape
+    with _here(dev):
+        if out is None:
+            out = {"loss": torch.empty(rows, dtype=torch.float32, device=dev), "lse": torch.empty(rows, dtype=torch.float32, device=dev)}
+        loss = _contiguous(out["loss"], "loss", torch.float32, rows, dev)
+        lse = _contiguous(out["lse"], "lse", torch.float32, rows, dev)
+        if rows == 0:
+            return out
+        ws = _workspace(workspace, lib().guard_linear_xent_workspace_bytes(rows, width, w.shape[0], 0), dev)
+        _check(lib().guard_linear_xent(x.data_ptr(), xs, w.data_ptr(), wst, rows, width, w.shape[0], code, targets.data_ptr(), bits, ignore_index,
+                                       loss, lse, ws.data_ptr(), ws.numel(), _status_ptr(out, dev), guard._stream()))
+    return out
+
+
+def linear_xent_grad(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, grad_loss: torch.Tensor, *,
+                     ignore_index: int = -100, workspace: Optional[torch.Tensor] = None,
+                     out: Optional[Dict[str, Optional[torch.Tensor]]] = None) -> Dict[str, Optional[torch.Tensor]]:
+    """Gradients of (grad_loss * loss).sum(): out["dx"] and out["dw"], of the inputs' type (a missing or None entry of `out`
+    is skipped).  lse: as linear_xent gave it; grad_loss: float32, one value per row, or one for all."""
+    dev, bits, code, xs, wst = _product(x, w, targets)
+    rows, width = x.shape
+    vocab = w.shape[0]
+    with _here(dev):
+        if out is None:
+            out = {"dx": torch.empty((rows, width), dtype=x.dtype, device=dev), "dw": torch.empty((vocab, width), dtype=w.dtype, device=dev)}
+        dx, dw = out.get("dx"), out.get("dw")
+        pdx = None if dx is None else _contiguous(dx, "dx", x.dtype, rows * width, dev)
+        pdw = None if dw is None else _contiguous(dw, "dw", w.dtype, vocab * width, dev)
+        plse = _contiguous(lse, "lse", torch.float32, rows, dev)
+        one = grad_loss.numel() == 1 and rows != 1
+        pg = _contiguous(grad_loss, "grad_loss", torch.float32, 1 if one else rows, dev)
+        ws = _workspace(workspace, lib().guard_linear_xent_workspace_bytes(rows, width, vocab, 1), dev) if rows else None
+        _check(lib().guard_linear_xent_grad(x.data_ptr(), xs, w.data_ptr(), wst, rows, width, vocab, code, targets.data_ptr(), bits, ignore_index,
+                                            plse, pg, 0 if one else 1, pdx, pdw, ws.data_ptr() if rows else None, ws.numel() if rows else 0,
+                                            _status_ptr(out, dev), guard._stream()))
     return out
 
 
