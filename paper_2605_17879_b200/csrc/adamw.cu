@@ -26,21 +26,20 @@ __device__ __forceinline__ double power(double b, int64_t n) {   // b^n by squar
 
 // 32 dithering bits of a position: two multiplicative rounds over position and key.  Neighbouring positions and steps
 // only have to be uncorrelated and each value equally frequent, which the tests count.
-__device__ __forceinline__ uint32_t dither(uint64_t i, uint32_t key) {
-    uint32_t h = ((uint32_t)i + (uint32_t)(i >> 32) * 0x85EBCA6Bu) ^ key;
-    h *= 0x9E3779B1u;
+__device__ __forceinline__ uint32_t dither(uint32_t i, uint32_t key) {
+    uint32_t h = (i ^ key) * 0x9E3779B1u;
     h ^= h >> 15;
     h *= 0x85EBCA77u;
     return h ^ (h >> 13);
 }
 
-// 0 <= y <= 448 to a multiple of e4m3's step there, up with the probability of what is cut off (16 random bits; the result
-// converts exactly).  Below 2^-6 the steps are 2^-9; `least`: a nonzero value is one step at least.
-__device__ __forceinline__ float to_step(float y, uint32_t bits, bool least) {
-    const float fine = __uint_as_float((__float_as_uint(y) + (bits << 4)) & ~0xFFFFFu);
-    float steps = floorf(__fadd_rn(__fmul_rn(y, 512.0f), __fmul_rn((float)bits, 1.0f / 65536.0f)));
-    if (least && y > 0.0f) steps = fmaxf(steps, 1.0f);
-    return y < 0.015625f ? __fmul_rn(steps, 1.0f / 512.0f) : fine;
+// y in [0, 448] to a multiple of e4m3's step there, up with the probability of what is cut off (16 random bits; the result
+// converts exactly): random bits are added below the three bits of fraction that stay, then cut off.  Below 2^-6 e4m3's
+// steps stay 2^-9, as they are in [2^-6, 2^-5): the value is moved there and back.
+__device__ __forceinline__ float to_step(float y, uint32_t bits) {
+    const float up = y < 0.015625f ? 0.015625f : 0.0f;
+    const float t = __fadd_rn(y, up);
+    return __fsub_rn(__uint_as_float((__float_as_uint(t) + (bits << 4)) & ~0xFFFFFu), up);
 }
 // Two values in e4m3, the first in the low byte.
 __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
@@ -56,9 +55,15 @@ __device__ __forceinline__ void from_e4m3x2(uint32_t two, float &lo, float &hi) 
     hi = __high2float(h);
 }
 
-__device__ __forceinline__ float warp_max(float x) {
-    for (int d = 16; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, d));
-    return x;
+__device__ __forceinline__ float root(float x) {
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+    float y;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 // Eight values of a lane; those behind `left` are zero.
@@ -120,23 +125,35 @@ __device__ __forceinline__ void load8_e4m3(const uint8_t *p, int left, float sca
 // step would round every value anew, and the noise of that adds up over the 1 / (1 - beta2) steps that a mean remembers.
 template <bool LEAST>
 __device__ __forceinline__ float store8_e4m3(uint8_t *p, int left, const float (&x)[8], const uint32_t (&bits)[8]) {
-    float top = 0.0f;
+    uint32_t top = 0;                          // magnitudes order as their bits do
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[j]));      // (a NaN leaves the others' scale alone)
-    const uint32_t high = (__float_as_uint(warp_max(top)) + 0x1FFFFFu) >> 23;
+    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    const bool strange = top >= 0x7F800000u;   // some value is not finite: it becomes NaN, the others keep a scale of their own
+    if (strange) {
+        top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, fabsf(x[j]) < INFINITY ? __float_as_uint(x[j]) & 0x7FFFFFFFu : 0u);
+        top = __reduce_max_sync(0xFFFFFFFFu, top);
+    }
+    const uint32_t high = (top + 0x1FFFFFu) >> 23;
     const uint32_t e = (high < 9 ? 9 : high) - 8;                     // the scale's exponent field, 1 .. 247
     const float inverse = __uint_as_float((254 - e) << 23);
+    float y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        y[j] = __fmul_rn(LEAST ? x[j] : fabsf(x[j]), inverse);         // (LEAST: second moments, never negative)
+        const float stepped = to_step(y[j], bits[j]);
+        y[j] = LEAST ? (y[j] > 0.0f ? fmaxf(stepped, 0.001953125f) : y[j]) : copysignf(stepped, x[j]);
+    }
+    if (strange) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (!(fabsf(x[j]) < INFINITY)) y[j] = __uint_as_float(0x7FC00000u);
+    }
     uint32_t w[2] = {0, 0};
 #pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-        float y[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float a = __fmul_rn(fabsf(x[j + h]), inverse);
-            y[h] = copysignf(a <= 448.0f ? to_step(a, bits[j + h], LEAST) : __uint_as_float(0x7FC00000u), x[j + h]);   // infinite: NaN
-        }
-        w[j >> 2] |= to_e4m3x2(y[0], y[1]) << (16 * ((j >> 1) & 1));
-    }
+    for (int j = 0; j < 8; j += 2) w[j >> 2] |= to_e4m3x2(y[j], y[j + 1]) << (16 * ((j >> 1) & 1));
     if (left >= 8) {
         asm volatile("st.global.L1::no_allocate.v2.b32 [%2], {%0,%1};" ::"r"(w[0]), "r"(w[1]), "l"(p) : "memory");
     } else {
@@ -147,19 +164,19 @@ __device__ __forceinline__ float store8_e4m3(uint8_t *p, int left, const float (
 
 template <typename G, typename Cp, int BITS>
 __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwArgs a) {
-    __shared__ float s_rate, s_shrink, s_lr;
+    __shared__ float s_rate, s_grow, s_lr;
     pdl_wait();
     const int64_t t = a.counter->step + 1;
     if (threadIdx.x == 0) {
         const double lr = a.d_lr ? (double)*a.d_lr : a.lr;
         s_rate = (float)(lr / (1.0 - power(a.dbeta1, t)));
-        s_shrink = (float)sqrt(1.0 - power(a.dbeta2, t));
+        s_grow = (float)(1.0 / sqrt(1.0 - power(a.dbeta2, t)));
         s_lr = (float)lr;
     }
     const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
     const uint32_t key = a.seed + (uint32_t)t * 0x9E3779B9u;
     __syncthreads();
-    const float rate = s_rate, shrink = s_shrink, lr = s_lr;
+    const float rate = s_rate, grow = s_grow, lr = s_lr;
     const int lane = lane_id(), warp = warp_id();
     const int64_t chunks = (a.blocks + kAdamwChunk - 1) / kAdamwChunk;
     for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
@@ -188,8 +205,9 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwArgs a) {
                 const float gj = __fmul_rn(g[j], gs);
                 m[j] = __fadd_rn(__fmul_rn(m[j], a.beta1), __fmul_rn(gj, a.rest1));
                 v[j] = __fadd_rn(__fmul_rn(v[j], a.beta2), __fmul_rn(__fmul_rn(gj, gj), a.rest2));
-                const float den = __fadd_rn(__fdiv_rn(__fsqrt_rn(v[j]), shrink), a.eps);
-                p[j] = __fsub_rn(__fmul_rn(p[j], keep), __fmul_rn(rate, __fdiv_rn(m[j], den)));
+                // root and reciprocal are good to 2^-23, on an update that is small against the parameter
+                const float den = __fadd_rn(__fmul_rn(root(v[j]), grow), a.eps);
+                p[j] = __fmaf_rn(p[j], keep, -__fmul_rn(rate, __fmul_rn(m[j], reciprocal(den))));
             }
             store8(T.param + at, left, wide, p);
             if (T.copy) store8(reinterpret_cast<Cp *>(T.copy) + at, left, wide, p);
@@ -198,10 +216,12 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwArgs a) {
                 store8(reinterpret_cast<float *>(a.v) + flat, left, true, v);
             } else {
                 uint32_t lo[8], hi[8];
+                // (eight positions from a multiple of eight on differ in the low word alone)
+                const uint32_t place = (uint32_t)flat + (uint32_t)(flat >> 32) * 0x85EBCA6Bu;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     if (j >= left) m[j] = v[j] = 0.0f;
-                    const uint32_t h = dither((uint64_t)(flat + j), key);
+                    const uint32_t h = dither(place + j, key);
                     lo[j] = h & 0xFFFFu;
                     hi[j] = h >> 16;
                 }

@@ -4,13 +4,15 @@
 //
 // Gradient: dtable[v] = scale * sum of the gradient rows of the positions with token v.  Summing with atomics would make
 // the order, and with it the result, a matter of chance, and would serialise on frequent tokens; so the positions are sorted
-// by token first (a stable radix sort), then every row of the table has one writer.
+// by token first (a stable radix sort), and runs of one token are summed.
 //   1. embed_sort_*: least significant digit first, kDigitBits at a time; a CTA ranks a tile of keys with warp matches and
 //      counters of its own, so equal keys keep their order.  One tile: all digits in one launch.  More: two launches per digit.
-//   2. embed_window_kernel: the first and last position of every token, and the sums of those windows of 64 sorted positions
-//      that belong to one token altogether, in float32, so that a token that occurs thousands of times is summed by many warps.
-//   3. embed_rows_kernel: a warp per row of the table adds its windows and the positions at both ends, or writes zeros.  A
-//      row of many windows is added by the whole CTA.
+//   2. embed_sum_kernel: a warp takes a window of 32 sorted positions and a strip of columns, loads 16 rows' vectors at a time
+//      and adds them run by run.  A run inside the window is a finished row.  One that crosses its borders leaves a partial
+//      sum: two places a window, in order, so the partial sums are again a sorted list, a sixteenth as long, to which the
+//      same kernel is applied until one window is left.  So a token that occurs once costs one read and one write, one that
+//      fills the batch is summed by as many warps as there are windows, and nothing depends on how frequent tokens are.
+//      The first of these launches also writes zeros to the rows without tokens (a bit per row, set while sorting).
 // The grouping of a sum depends on the positions alone.
 #include "train_ops.h"
 
@@ -24,10 +26,12 @@ constexpr int kSortThreads = 512;            // one per digit in the scans
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortItems = 4;                // keys a thread ranks at a time
 constexpr int kTile = kSortThreads * kSortItems;
-constexpr int kWindow = 64;
-constexpr int kRowThreads = 256;
-constexpr int kRowWarps = kRowThreads / 32;
-constexpr int kCols = 8;                     // columns a lane holds at a time
+constexpr int kWindow = 32;
+constexpr int kBatch = 16;                   // rows whose vectors are loaded together
+constexpr int kSumThreads = 256;
+constexpr int kSumWarps = kSumThreads / 32;
+constexpr uint32_t kHole = 0x80000000u;      // a place without a partial sum; its key keeps the list sorted
+constexpr int kCols = 8;                     // columns a thread of the lookup copies
 
 __device__ __forceinline__ int64_t token_at(const void *tokens, int bits, int64_t i) {
     return bits == 64 ? __ldg(reinterpret_cast<const long long *>(tokens) + i) : (int64_t)__ldg(reinterpret_cast<const int *>(tokens) + i);
@@ -108,14 +112,15 @@ struct SortShared {
     uint32_t scan[kSortWarps];
 };
 
-// A position's key: its token, or `rows` (behind all tokens) where it adds nothing.
-__device__ __forceinline__ uint32_t key_at(const EmbedGradArgs &a, int64_t i) {
+// A position's key: its token, or `rows` (behind all tokens) where it adds nothing.  Sets the token's bit.
+__device__ __forceinline__ uint32_t key_at(const EmbedGradArgs &a, uint32_t *present, int64_t i) {
     const int64_t t = token_at(a.tokens, a.token_bits, i);
     if (t == a.padding) return (uint32_t)a.rows;
     if (t < 0 || t >= a.rows) {
         if (a.status) atomicOr(a.status, kStatIndex);
         return (uint32_t)a.rows;
     }
+    if (present) atomicOr(present + (t >> 5), 1u << (t & 31));
     return (uint32_t)t;
 }
 
@@ -170,22 +175,18 @@ __device__ __forceinline__ uint32_t digits_before(SortShared &s, uint32_t mine) 
     return before + x - mine;
 }
 
-__device__ __forceinline__ void clear_bounds(uint2 *bounds, int64_t rows) {
-    for (int64_t v = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; v < rows; v += (int64_t)gridDim.x * kSortThreads) bounds[v] = make_uint2(0, 0);
-}
-
 struct SortArgs {
     EmbedGradArgs a;
     const uint32_t *in_key, *in_pos;   // the previous digit's order (unused for the first digit)
     uint32_t *out_key, *out_pos;
     uint32_t *counts;                  // [tiles][kDigits]
-    uint2 *bounds;
+    uint32_t *present;                 // a bit per row of the table: some position has its token
     int64_t tiles;
     int shift, digits, first;
 };
 
 __device__ __forceinline__ void load_tile(const SortArgs &s, int64_t tile, uint32_t (&key)[kSortItems], uint32_t (&pos)[kSortItems],
-                                          bool (&have)[kSortItems]) {
+                                          bool (&have)[kSortItems], bool mark) {
     const int64_t at = tile * kTile + (int64_t)warp_id() * (32 * kSortItems) + lane_id();
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
@@ -194,7 +195,7 @@ __device__ __forceinline__ void load_tile(const SortArgs &s, int64_t tile, uint3
         key[r] = 0;
         pos[r] = 0;
         if (have[r]) {
-            key[r] = s.first ? key_at(s.a, i) : s.in_key[i];
+            key[r] = s.first ? key_at(s.a, mark ? s.present : nullptr, i) : s.in_key[i];
             pos[r] = s.first ? (uint32_t)i : s.in_pos[i];
         }
     }
@@ -208,13 +209,12 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_count_kernel(const So
     __syncthreads();
     uint32_t key[kSortItems], pos[kSortItems];
     bool have[kSortItems];
-    load_tile(s, blockIdx.x, key, pos, have);
+    load_tile(s, blockIdx.x, key, pos, have, true);
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r)
         if (have[r]) atomicAdd(&count[(key[r] >> s.shift) & (kDigits - 1)], 1u);
     __syncthreads();
     s.counts[(int64_t)blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
-    if (s.first) clear_bounds(s.bounds, s.a.rows);
 }
 
 // Moves a tile's keys to their places in the digit's order.
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_move_kernel(const Sor
     pdl_wait();
     uint32_t key[kSortItems], pos[kSortItems], rank[kSortItems];
     bool have[kSortItems];
-    load_tile(s, blockIdx.x, key, pos, have);
+    load_tile(s, blockIdx.x, key, pos, have, false);
     rank_tile(sh, key, have, s.shift, rank);
     warps_before(sh);
     uint32_t all = 0, mine = 0;
@@ -244,16 +244,16 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_move_kernel(const Sor
         }
 }
 
-// One tile: every digit in turn by one CTA; the others clear the bounds.
+// One tile: every digit in turn by one CTA.
 __global__ void __launch_bounds__(kSortThreads) embed_sort_tile_kernel(const SortArgs s) {
     __shared__ SortShared sh;
     __shared__ uint32_t keys[kTile], places[kTile];
     pdl_wait();
-    clear_bounds(s.bounds, s.a.rows);
-    if (blockIdx.x != 0) return;
+    for (int64_t v = threadIdx.x; v < (s.a.rows + 31) / 32; v += kSortThreads) s.present[v] = 0;
+    __syncthreads();
     uint32_t key[kSortItems], pos[kSortItems], rank[kSortItems];
     bool have[kSortItems];
-    load_tile(s, 0, key, pos, have);
+    load_tile(s, 0, key, pos, have, true);
     for (int d = 0; d < s.digits; ++d) {
         const int shift = d * kDigitBits;
         rank_tile(sh, key, have, shift, rank);
@@ -287,148 +287,174 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_tile_kernel(const Sor
         }
 }
 
+__global__ void __launch_bounds__(256) embed_clear_kernel(uint32_t *p, int64_t n) {
+    pdl_wait();
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
+}
+
 // ---- sums ------------------------------------------------------------------------------------------------------------
 
 struct SumArgs {
-    EmbedGradArgs a;
-    const uint32_t *key, *pos;   // sorted
-    uint2 *bounds;               // [rows] first and end of a token's sorted positions
-    float *windows;              // [n / kWindow][width] sums of windows of one token
-    bool wide;
+    int64_t n;                   // length of the list
+    const uint32_t *key, *pos;   // sorted keys (kHole: nothing there); positions (first list only)
+    const void *from;            // gradient rows, or partial sums by place in the list
+    int64_t stride;
+    uint32_t *next_key;          // the list of partial sums, two places a window
+    float *next;
+    int64_t rows, width;
+    float scale;
+    int accumulate;
+    void *dtable;
+    const uint32_t *present;     // first list, where rows without tokens become zero; else NULL
+    unsigned sum_blocks;
+    int strips;
 };
 
-// Adds the gradient rows of sorted positions [from, to) to x, columns col .. col + 7, in order.
-template <typename T>
-__device__ __forceinline__ void add_rows(const SumArgs &s, uint32_t from, uint32_t to, int64_t col, int left, float (&x)[kCols]) {
-    const T *g = reinterpret_cast<const T *>(s.a.grad) + col;
-    uint32_t i = from;
-    for (; i + 4 <= to; i += 4) {
-        float y[4][kCols];
+// The lane's columns of a strip of 32 * V columns: V consecutive ones (WIDE: one vector of 16 bytes of the rows' type), or
+// every 32nd.
+template <bool WIDE, int V> __device__ __forceinline__ int64_t column(int64_t strip, int j) {
+    return WIDE ? (strip * 32 + lane_id()) * V + j : strip * 32 * V + j * 32 + lane_id();
+}
+template <typename T, bool WIDE, int V>
+__device__ __forceinline__ void load_strip(const T *row, int64_t strip, int64_t width, T (&x)[V]) {
+    if constexpr (WIDE) {
+        static_assert(sizeof(T) * V == 16, "");
+        const int64_t c = column<true, V>(strip, 0);
+        if (c < width) *reinterpret_cast<uint4 *>(x) = *reinterpret_cast<const uint4 *>(row + c);
+    } else {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) load_cols(g + (int64_t)s.pos[i + u] * s.a.stride, left, s.wide, y[u]);
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int j = 0; j < kCols; ++j) x[j] = __fadd_rn(x[j], y[u][j]);
+        for (int j = 0; j < V; ++j) {
+            const int64_t c = column<false, V>(strip, j);
+            if (c < width) x[j] = row[c];
+        }
     }
-    for (; i < to; ++i) {
-        float y[kCols];
-        load_cols(g + (int64_t)s.pos[i] * s.a.stride, left, s.wide, y);
+}
+template <typename O, bool WIDE, int V>
+__device__ __forceinline__ void store_strip(O *row, int64_t strip, int64_t width, const float (&x)[V]) {
+    if constexpr (WIDE) {
+        const int64_t c = column<true, V>(strip, 0);
+        if (c >= width) return;
+        O y[V];
 #pragma unroll
-        for (int j = 0; j < kCols; ++j) x[j] = __fadd_rn(x[j], y[j]);
+        for (int j = 0; j < V; ++j) y[j] = Conv<O>::down(x[j]);
+        constexpr int B = sizeof(O) * V;          // 8, 16 or 32 bytes
+        if constexpr (B == 8) *reinterpret_cast<uint2 *>(row + c) = *reinterpret_cast<const uint2 *>(y);
+        else
+#pragma unroll
+            for (int h = 0; h < B / 16; ++h) reinterpret_cast<uint4 *>(row + c)[h] = reinterpret_cast<const uint4 *>(y)[h];
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int64_t c = column<false, V>(strip, j);
+            if (c < width) row[c] = Conv<O>::down(x[j]);
+        }
     }
 }
 
-// A warp per window of sorted positions: notes where tokens begin and end, and sums the window if it is one token's.
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) embed_window_kernel(const SumArgs s) {
+// Zeros for the rows of the table without tokens; a warp looks at 32 rows at a time.
+template <typename O, bool WIDE>
+__device__ __forceinline__ void clear_rows(const SumArgs &s, int64_t warp, int64_t warps) {
+    O *table = reinterpret_cast<O *>(s.dtable);
+    const int64_t words = (s.rows + 31) / 32;
+    for (int64_t w = warp; w < words; w += warps) {
+        const uint32_t bits = s.present[w];
+        const int rows = (int)min((int64_t)32, s.rows - w * 32);
+        for (int r = 0; r < rows; ++r) {
+            if ((bits >> r) & 1) continue;
+            O *row = table + (w * 32 + r) * s.width;
+            if constexpr (WIDE) {
+                constexpr int V = 16 / sizeof(O);
+                for (int64_t c = lane_id() * V; c < s.width; c += 32 * V) *reinterpret_cast<uint4 *>(row + c) = make_uint4(0, 0, 0, 0);
+            } else {
+                for (int64_t c = lane_id(); c < s.width; c += 32) row[c] = Conv<O>::down(0.0f);
+            }
+        }
+    }
+}
+
+// T: the list's rows (the gradient's type, or float32 for partial sums); O: the table's.
+template <typename T, typename O, bool WIDE>
+__global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const SumArgs s) {
+    constexpr int V = 16 / sizeof(T);
     pdl_wait();
-    const int64_t windows = (s.a.n + kWindow - 1) / kWindow;
-    const uint32_t n = (uint32_t)s.a.n, rows = (uint32_t)s.a.rows;
-    for (int64_t w = (int64_t)blockIdx.x * kRowWarps + warp_id(); w < windows; w += (int64_t)gridDim.x * kRowWarps) {
-        const uint32_t from = (uint32_t)w * kWindow;
+    const int lane = lane_id();
+    if (blockIdx.x >= s.sum_blocks) {
+        clear_rows<O, WIDE>(s, (int64_t)(blockIdx.x - s.sum_blocks) * kSumWarps + warp_id(), (int64_t)(gridDim.x - s.sum_blocks) * kSumWarps);
+        return;
+    }
+    const int64_t windows = (s.n + kWindow - 1) / kWindow, work = windows * s.strips;
+    for (int64_t u = (int64_t)blockIdx.x * kSumWarps + warp_id(); u < work; u += (int64_t)s.sum_blocks * kSumWarps) {
+        const int64_t w = u / s.strips, strip = u - w * s.strips;
+        const int64_t i = w * kWindow + lane;
+        const uint32_t raw = i < s.n ? s.key[i] : 0x7FFFFFFFu;
+        const uint32_t key = raw & ~kHole;
+        const uint32_t pos = s.pos && i < s.n ? s.pos[i] : (uint32_t)i;
+        const uint32_t used = __ballot_sync(0xFFFFFFFFu, raw == key && key < (uint32_t)s.rows);
+        const uint32_t before = w > 0 ? s.key[w * kWindow - 1] & ~kHole : 0x7FFFFFFFu;
+        const uint32_t after = (w + 1) * kWindow < s.n ? s.key[(w + 1) * kWindow] & ~kHole : 0x7FFFFFFFu;
+        const uint32_t next = __shfl_down_sync(0xFFFFFFFFu, key, 1);
+        // where a run ends; the last one of the window may go on
+        const uint32_t ends = __ballot_sync(0xFFFFFFFFu, lane == 31 || next != key);
+        const uint32_t first = __shfl_sync(0xFFFFFFFFu, key, 0), last = __shfl_sync(0xFFFFFFFFu, key, 31);
+        const bool enters = first == before, leaves = last == after;
+        float sum[V] = {};
+        bool any = false, head = true;            // the run holds something; it is the window's first
+        bool full0 = false, full1 = false;        // places of the next list that get a partial sum
 #pragma unroll
-        for (int h = 0; h < kWindow; h += 32) {
-            const uint32_t i = from + h + lane_id();
-            if (i < n) {
-                const uint32_t k = s.key[i];
-                if (k < rows) {
-                    if (i == 0 || s.key[i - 1] != k) s.bounds[k].x = i;
-                    if (i == n - 1 || s.key[i + 1] != k) s.bounds[k].y = i + 1;
+        for (int b = 0; b < kWindow; b += kBatch) {
+            T x[kBatch][V];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const uint32_t p = __shfl_sync(0xFFFFFFFFu, pos, b + j);
+                if ((used >> (b + j)) & 1) load_strip<T, WIDE, V>(reinterpret_cast<const T *>(s.from) + (int64_t)p * s.stride, strip, s.width, x[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                if ((used >> (b + j)) & 1) {
+                    any = true;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) sum[e] = __fadd_rn(sum[e], Conv<T>::up(x[j][e]));
+                }
+                if ((ends >> (b + j)) & 1) {
+                    const bool tail = b + j == 31 && leaves, from_before = head && enters;
+                    if (any) {
+                        if (tail || from_before) {
+                            const int at = from_before ? 0 : 1;
+                            full0 |= from_before;
+                            full1 |= !from_before;
+                            store_strip<float, WIDE, V>(s.next + (2 * w + at) * s.width, strip, s.width, sum);
+                        } else {
+                            const uint32_t row = __shfl_sync(0xFFFFFFFFu, key, b + j);
+                            O *out = reinterpret_cast<O *>(s.dtable) + (int64_t)row * s.width;
+#pragma unroll
+                            for (int e = 0; e < V; ++e) sum[e] = __fmul_rn(sum[e], s.scale);
+                            if (s.accumulate) {
+#pragma unroll
+                                for (int e = 0; e < V; ++e) {
+                                    const int64_t c = column<WIDE, V>(strip, e);
+                                    if (c < s.width) sum[e] = __fadd_rn(Conv<O>::up(out[c]), sum[e]);
+                                }
+                            }
+                            store_strip<O, WIDE, V>(out, strip, s.width, sum);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < V; ++e) sum[e] = 0.0f;
+                    any = head = false;
                 }
             }
         }
-        if (from + kWindow > n) continue;
-        const uint32_t k = s.key[from];
-        if (k >= rows || s.key[from + kWindow - 1] != k) continue;
-        for (int64_t col = lane_id() * kCols; col < s.a.width; col += 32 * kCols) {
-            const int left = (int)min((int64_t)kCols, s.a.width - col);
-            float x[kCols] = {};
-            add_rows<T>(s, from, from + kWindow, col, left, x);
-            store_cols(s.windows + w * s.a.width + col, left, s.a.width % 4 == 0, x);
-        }
-    }
-}
-
-// Adds window sums [w0, w1) to x.
-__device__ __forceinline__ void add_windows(const SumArgs &s, uint32_t w0, uint32_t w1, int64_t col, int left, float (&x)[kCols]) {
-    const bool wide = s.a.width % 4 == 0;
-    uint32_t w = w0;
-    for (; w + 4 <= w1; w += 4) {
-        float y[4][kCols];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) load_cols(s.windows + (int64_t)(w + u) * s.a.width + col, left, wide, y[u]);
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int j = 0; j < kCols; ++j) x[j] = __fadd_rn(x[j], y[u][j]);
-    }
-    for (; w < w1; ++w) {
-        float y[kCols];
-        load_cols(s.windows + (int64_t)w * s.a.width + col, left, wide, y);
-#pragma unroll
-        for (int j = 0; j < kCols; ++j) x[j] = __fadd_rn(x[j], y[j]);
-    }
-}
-
-// One row, columns from the lane's first on, `step` columns apart.
-template <typename T>
-__device__ __forceinline__ void sum_row(const SumArgs &s, int64_t v, uint2 b, int64_t col0, int64_t step) {
-    T *out = reinterpret_cast<T *>(s.a.dtable) + v * s.a.width;
-    // whole windows of this token: [w0, w1); the positions outside them at both ends
-    uint32_t w0 = (b.x + kWindow - 1) / kWindow, w1 = b.y / kWindow;
-    if (w1 <= w0) w0 = w1 = 0;
-    for (int64_t col = col0; col < s.a.width; col += step) {
-        const int left = (int)min((int64_t)kCols, s.a.width - col);
-        float x[kCols] = {};
-        if (w1 > w0) {
-            add_rows<T>(s, b.x, w0 * kWindow, col, left, x);
-            add_windows(s, w0, w1, col, left, x);
-            add_rows<T>(s, w1 * kWindow, b.y, col, left, x);
-        } else {
-            add_rows<T>(s, b.x, b.y, col, left, x);
-        }
-#pragma unroll
-        for (int j = 0; j < kCols; ++j) x[j] = __fmul_rn(x[j], s.a.scale);
-        if (s.a.accumulate) {
-            float y[kCols];
-            load_cols(out + col, left, s.wide, y);
-#pragma unroll
-            for (int j = 0; j < kCols; ++j) x[j] = __fadd_rn(y[j], x[j]);
-        }
-        store_cols(out + col, left, s.wide, x);
-    }
-}
-
-constexpr uint32_t kHeavy = 8 * kWindow;   // positions from which on a whole CTA adds a row
-
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) embed_rows_kernel(const SumArgs s) {
-    __shared__ uint2 s_bounds[kRowWarps];
-    pdl_wait();
-    const int64_t groups = (s.a.rows + kRowWarps - 1) / kRowWarps;
-    for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
-        const int64_t v = g * kRowWarps + warp_id();
-        const uint2 b = v < s.a.rows ? s.bounds[v] : make_uint2(0, 0);
-        const bool heavy = b.y - b.x >= kHeavy;
-        if (v < s.a.rows && !heavy && (b.y > b.x || !s.a.accumulate)) sum_row<T>(s, v, b, lane_id() * kCols, 32 * kCols);
-        if (__syncthreads_or(heavy)) {
-            if (lane_id() == 0) s_bounds[warp_id()] = b;
-            __syncthreads();
-            for (int r = 0; r < kRowWarps; ++r)
-                if (s_bounds[r].y - s_bounds[r].x >= kHeavy)
-                    sum_row<T>(s, g * kRowWarps + r, s_bounds[r], (int64_t)threadIdx.x * kCols, kRowThreads * kCols);
-            __syncthreads();
-        }
+        if (strip == 0 && lane < 2 && s.next_key) s.next_key[2 * w + lane] = (lane == 0 ? first : last) | ((lane == 0 ? full0 : full1) ? 0u : kHole);
     }
 }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct GradLayout {
-    size_t key[2], pos[2], counts, bounds, windows, total;
+    size_t key[2], pos[2], counts, present, next_key[2], next[2], total;
     int64_t tiles;
 };
+inline int64_t next_length(int64_t n) { return 2 * ((n + kWindow - 1) / kWindow); }
 GradLayout grad_layout(int64_t n, int64_t rows, int64_t width) {
     GradLayout L{};
     size_t off = 0;
@@ -438,24 +464,51 @@ GradLayout grad_layout(int64_t n, int64_t rows, int64_t width) {
         L.pos[i] = off, off = up256(off + (size_t)n * 4);
     }
     L.counts = off, off = up256(off + (size_t)L.tiles * kDigits * 4);
-    L.bounds = off, off = up256(off + (size_t)rows * sizeof(uint2));
-    L.windows = off, off = up256(off + (size_t)(n / kWindow) * width * 4);
+    L.present = off, off = up256(off + (size_t)((rows + 31) / 32) * 4);
+    // two lists of partial sums, used in turn
+    int64_t m = n > kWindow ? next_length(n) : 0;
+    for (int i = 0; i < 2; ++i) {
+        L.next_key[i] = off, off = up256(off + (size_t)m * 4);
+        L.next[i] = off, off = up256(off + (size_t)m * width * 4);
+        m = m > kWindow ? next_length(m) : 0;
+    }
     L.total = off ? off : 256;
     return L;
 }
 
+template <typename T, typename O>
+cudaError_t launch_sum(SumArgs s, bool wide, cudaStream_t st) {
+    const int64_t most = (int64_t)sm_count() * 8;
+    constexpr int V = 16 / sizeof(T);
+    s.strips = (int)((s.width + 32 * V - 1) / (32 * V));
+    const int64_t work = (s.n + kWindow - 1) / kWindow * s.strips;
+    int64_t blocks = (work + kSumWarps - 1) / kSumWarps;
+    if (blocks > most * 16) blocks = most * 16;
+    s.sum_blocks = (unsigned)blocks;
+    int64_t clear = s.present ? (s.rows + 32 * kSumWarps - 1) / (32 * kSumWarps) : 0;
+    if (clear > most) clear = most;
+    if (blocks + clear == 0) return cudaSuccess;
+    const dim3 grid((unsigned)(blocks + clear)), block(kSumThreads);
+    return wide ? launch_after(embed_sum_kernel<T, O, true>, grid, block, st, s) : launch_after(embed_sum_kernel<T, O, false>, grid, block, st, s);
+}
+
+// Sums the sorted list, then the lists of partial sums.
 template <typename T>
-cudaError_t launch_sums(const SumArgs &s, cudaStream_t st) {
-    const int64_t sms = sm_count();
-    const int64_t windows = (s.a.n + kWindow - 1) / kWindow;
-    int64_t grid = (windows + kRowWarps - 1) / kRowWarps;
-    if (grid > sms * 8) grid = sms * 8;
-    if (grid < 1) grid = 1;
-    cudaError_t e = launch_after(embed_window_kernel<T>, dim3((unsigned)grid), dim3(kRowThreads), st, s);
-    if (e != cudaSuccess) return e;
-    grid = (s.a.rows + kRowWarps - 1) / kRowWarps;
-    if (grid > sms * 8) grid = sms * 8;
-    return launch_after(embed_rows_kernel<T>, dim3((unsigned)grid), dim3(kRowThreads), st, s);
+cudaError_t launch_sums(SumArgs s, const GradLayout &L, char *ws, bool wide, cudaStream_t st) {
+    for (int level = 0;; ++level) {
+        const bool last = s.n <= kWindow;
+        const int to = level & 1;
+        s.next_key = last ? nullptr : (uint32_t *)(ws + L.next_key[to]);
+        s.next = last ? nullptr : (float *)(ws + L.next[to]);
+        const cudaError_t e = level == 0 ? launch_sum<T, T>(s, wide, st) : launch_sum<float, T>(s, wide, st);
+        if (e != cudaSuccess || last) return e;
+        s.n = next_length(s.n);
+        s.key = s.next_key;
+        s.from = s.next;
+        s.pos = nullptr;
+        s.stride = s.width;
+        s.present = nullptr;
+    }
 }
 
 bool aligned(const void *p, size_t to) { return (uintptr_t)p % to == 0; }
@@ -482,7 +535,7 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
     SortArgs s{};
     s.a = a;
     s.counts = (uint32_t *)(ws + L.counts);
-    s.bounds = (uint2 *)(ws + L.bounds);
+    s.present = (uint32_t *)(ws + L.present);
     s.tiles = L.tiles;
     int bits = 1;
     while (bits < 32 && (a.rows >> bits) != 0) ++bits;      // keys 0 .. rows
@@ -493,11 +546,12 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
         s.first = 1;
         s.out_key = (uint32_t *)(ws + L.key[0]);
         s.out_pos = (uint32_t *)(ws + L.pos[0]);
-        const int64_t clear = (a.rows + kSortThreads * 4 - 1) / (kSortThreads * 4);
-        const int64_t most = sm_count();
-        e = launch_after(embed_sort_tile_kernel, dim3((unsigned)(clear < 1 ? 1 : clear > most ? most : clear)), dim3(kSortThreads), st, s);
+        e = launch_after(embed_sort_tile_kernel, dim3(1), dim3(kSortThreads), st, s);
         if (e != cudaSuccess) return e;
     } else {
+        const int64_t words = (a.rows + 31) / 32, blocks = (words + 255) / 256;
+        e = launch_after(embed_clear_kernel, dim3((unsigned)(blocks < sm_count() ? blocks : sm_count())), dim3(256), st, s.present, words);
+        if (e != cudaSuccess) return e;
         for (int d = 0; d < s.digits; ++d) {
             s.first = d == 0;
             s.shift = d * kDigitBits;
@@ -513,14 +567,22 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
         }
     }
     SumArgs u{};
-    u.a = a;
+    u.n = a.n;
     u.key = (const uint32_t *)(ws + L.key[at]);
     u.pos = (const uint32_t *)(ws + L.pos[at]);
-    u.bounds = s.bounds;
-    u.windows = (float *)(ws + L.windows);
+    u.from = a.grad;
+    u.stride = a.stride;
+    u.rows = a.rows;
+    u.width = a.width;
+    u.scale = a.scale;
+    u.accumulate = a.accumulate;
+    u.dtable = a.dtable;
+    u.present = a.accumulate ? nullptr : s.present;
     const size_t b = dtype_bytes(dtype);
-    u.wide = aligned(a.grad, 16) && aligned(a.dtable, 16) && (a.width * b) % 16 == 0 && (a.stride * b) % 16 == 0;
-    return dtype == 0 ? launch_sums<float>(u, st) : dtype == 1 ? launch_sums<__nv_bfloat16>(u, st) : launch_sums<__half>(u, st);
+    const bool wide = aligned(a.grad, 16) && aligned(a.dtable, 16) && (a.width * b) % 16 == 0 && (a.stride * b) % 16 == 0;
+    return dtype == 0   ? launch_sums<float>(u, L, ws, wide, st)
+           : dtype == 1 ? launch_sums<__nv_bfloat16>(u, L, ws, wide, st)
+                        : launch_sums<__half>(u, L, ws, wide, st);
 }
 
 }  // namespace guard

@@ -11,9 +11,10 @@
 // Bound: the tensor cores, 2 N V D operations per product, but for few rows, where reading w once is what takes the time.
 //
 // Rounding: G is held in the inputs' type, since the tensor cores take both operands in one type; each value is off by at
-// most half a step (relative), as independent of its neighbours as the outputs' own rounding.  In float16 it is scaled by a
-// power of two that brings the largest |g_n| to [2^14, 2^15): exp(z - lse) below 2^-28 of that is lost, and the subnormal
-// range otherwise would be.  Sums are float32.
+// most half a step (relative), as independent of its neighbours as the outputs' own rounding.  It is held relative to the
+// largest |g_n|: where all rows weigh the same, as in a mean, the large value of a row, exp(z - lse) - 1 at its target,
+// then rounds from near -1 and not from -g_n, whose rounding error all rows would share.  In float16 it is scaled by 2^15
+// on top, or exp(z - lse) would lie among the subnormals; below 2^-39 it is lost.  Sums are float32.
 //
 // Rows that are ignored take no part: where there are any, the others are gathered first, and whatever the ignored ones
 // hold (NaN among it) reaches nothing.
@@ -35,14 +36,13 @@ constexpr int kEpilogueWarps = 8;
 constexpr int kProductThreads = 32 * (4 + kEpilogueWarps);
 constexpr int kProductSmem = kStages * (kABytes + kBBytes) + 1024;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kPart = kN / 2;                 // columns behind one partial result of a row: half a tile
 
 enum Mode { kStats, kGrad, kDx, kDw };
 
 struct Header {         // at the start of the workspace, written by xent_rows_kernel
     int32_t count;      // rows that take part
     int32_t whole;      // they are all rows: x is read where it is
-    float scale, inverse;   // of G, and what a gradient is multiplied by
+    float inverse;      // what a gradient from G is multiplied by
 };
 
 struct ProductArgs {
@@ -381,7 +381,7 @@ struct RowsArgs {
     const float *lse, *grad;   // backward: by row
     int64_t grad_stride;       // 0: one value for all rows
     float *lse_to, *grad_to;   // by gathered row
-    bool half;             // scale the row gradients for float16
+    bool grads, half;      // backward; float16
     float *loss, *lse_out; // forward: by row, written for those that take no part
     uint32_t *status;
 };
@@ -396,8 +396,8 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a) {
     __shared__ float s_top[32];
     pdl_wait();
     const int lane = lane_id(), warp = warp_id();
-    float scale = 1.0f, inverse = 1.0f;
-    if (a.half) {                      // a power of two that brings the largest |g| to [2^14, 2^15)
+    float unit = 1.0f, scale = 1.0f;      // G holds g / unit * scale
+    if (a.grads) {
         float top = 0.0f;
         for (int i = threadIdx.x; i < a.rows; i += 1024) {
             const int64_t t = target_at(a.targets, a.bits, i);
@@ -407,12 +407,9 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a) {
         if (lane == 0) s_top[warp] = top;
         __syncthreads();
         for (int w = 0; w < 32; ++w) top = fmaxf(top, s_top[w]);
-        if (top > 0.0f && top < INFINITY) {
-            int e;
-            frexpf(top, &e);           // top in [2^(e-1), 2^e)
-            e = min(max(15 - e, -120), 120);
-            scale = ldexpf(1.0f, e);
-            inverse = ldexpf(1.0f, -e);
+        if (top >= 1e-30f && top < INFINITY) {     // (else the products below could leave float32's range)
+            unit = top;
+            if (a.half) scale = 32768.0f;
         }
     }
     int before = 0;
@@ -444,7 +441,7 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a) {
             a.row_of[at] = (int32_t)i;
             if (a.lse_to) {
                 a.lse_to[at] = a.lse[i];
-                a.grad_to[at] = __fmul_rn(a.grad[i * a.grad_stride], scale);
+                a.grad_to[at] = __fmul_rn(__fdiv_rn(a.grad[i * a.grad_stride], unit), scale);
             }
         }
         if (i < a.rows) a.place[i] = in ? at : -1;
@@ -454,8 +451,7 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a) {
     if (threadIdx.x == 0) {
         a.head->count = before;
         a.head->whole = before == a.rows;
-        a.head->scale = scale;
-        a.head->inverse = inverse;
+        a.head->inverse = __fdiv_rn(unit, scale);
     }
 }
 
@@ -702,6 +698,7 @@ cudaError_t launch_rows(const XentArgs &x, const XentLayout &L, bool grads, cuda
         r.grad_stride = x.grad_stride;
         r.lse_to = (float *)(ws + L.lse);
         r.grad_to = (float *)(ws + L.grad);
+        r.grads = true;
         r.half = x.dtype == 2;
     } else {
         r.loss = x.loss;

@@ -64,13 +64,13 @@ def check_forward(out, ref, d):
     assert ((out["loss"].double() - ref["loss"]).abs() <= 2 * tol + U32 * ref["loss"].abs()).all()
 
 
-def check_grads(out, ref, d, n, v, dtype):
+def check_grads(out, ref, grad, d, n, v, dtype):
     h = HALF[dtype]
     rel = 3 * ((d / 16 + 16) * 2 * U32 * ref["big"] + 2.0 ** -20)[:, None]     # of exp(z - lse): logit, log sum and exponential
-    # G: that of its exponential, and one rounding to the inputs' type; in float16 also what lies below its subnormals
-    # relative to the largest |grad| (2^-25 of its smallest step against 2^14)
-    top = ref["G"].abs().max() if dtype == torch.float16 else 0.0
-    gerr = ref["P"] * rel + ref["G"].abs() * h + top * 2.0 ** -38
+    # G: that of its exponential, two float32 roundings of its row's weight, and one to the inputs' type; in float16 also
+    # half a smallest step, 2^-25, relative to 2^15 times the largest weight
+    top = grad.abs().max().double() if dtype == torch.float16 else 0.0
+    gerr = ref["P"] * rel + ref["G"].abs() * (h + 4 * U32) + top * 2.0 ** -40
     for name, err, size, want, depth in (("dx", gerr @ ref["w"].abs(), ref["G"].abs() @ ref["w"].abs(), ref["dx"], v),
                                          ("dw", gerr.T @ ref["x"].abs(), ref["G"].abs().T @ ref["x"].abs(), ref["dw"], n)):
         tol = (err + (depth / 16 + 16) * 2 * U32 * size) * 1.01 + want.abs() * h * 1.01 + TINY[dtype]
@@ -94,7 +94,7 @@ def test_loss_and_gradients(ops, dtype, n, d, v, ignored, pad):
         check_forward(out, ref, d)
         back = ops.linear_xent_grad(x, w, targets, out["lse"], grad)
         ops.sync_status()
-        check_grads(back, ref, d, n, v, dtype)
+        check_grads(back, ref, grad, d, n, v, dtype)
     again = ops.linear_xent_grad(x, w, t, out["lse"], grad)
     assert torch.equal(again["dx"], back["dx"]) and torch.equal(again["dw"], back["dw"])     # bit for bit
     assert torch.equal(ops.linear_xent(x, w, t)["loss"], out["loss"])
