@@ -36,10 +36,10 @@ __device__ __forceinline__ uint32_t dither(uint32_t i, uint32_t key) {
 // y in [0, 448] to a multiple of e4m3's step there, up with the probability of what is cut off (16 random bits; the result
 // converts exactly): random bits are added below the three bits of fraction that stay, then cut off.  Below 2^-6 e4m3's
 // steps stay 2^-9, as they are in [2^-6, 2^-5): the value is moved there and back.
-__device__ __forceinline__ float to_step(float y, uint32_t bits) {
+__device__ __forceinline__ float to_step(float y, uint32_t bits20) {   // (the 16 bits in the upper part of 20)
     const float up = y < 0.015625f ? 0.015625f : 0.0f;
     const float t = __fadd_rn(y, up);
-    return __fsub_rn(__uint_as_float((__float_as_uint(t) + (bits << 4)) & ~0xFFFFFu), up);
+    return __fsub_rn(__uint_as_float((__float_as_uint(t) + bits20) & ~0xFFFFFu), up);
 }
 // Two values in e4m3, the first in the low byte.
 __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
@@ -57,12 +57,12 @@ __device__ __forceinline__ void from_e4m3x2(uint32_t two, float &lo, float &hi) 
 
 __device__ __forceinline__ float root(float x) {
     float y;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ float reciprocal(float x) {
     float y;
-    asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
@@ -127,7 +127,7 @@ template <bool LEAST>
 __device__ __forceinline__ float store8_e4m3(uint8_t *p, int left, const float (&x)[8], const uint32_t (&bits)[8]) {
     uint32_t top = 0;                          // magnitudes order as their bits do
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+    for (int j = 0; j < 8; ++j) top = max(top, LEAST ? __float_as_uint(x[j]) : __float_as_uint(x[j]) & 0x7FFFFFFFu);   // (LEAST: second moments, never negative)
     top = __reduce_max_sync(0xFFFFFFFFu, top);
     const bool strange = top >= 0x7F800000u;   // some value is not finite: it becomes NaN, the others keep a scale of their own
     if (strange) {
@@ -142,7 +142,7 @@ __device__ __forceinline__ float store8_e4m3(uint8_t *p, int left, const float (
     float y[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        y[j] = __fmul_rn(LEAST ? x[j] : fabsf(x[j]), inverse);         // (LEAST: second moments, never negative)
+        y[j] = __fmul_rn(LEAST ? x[j] : fabsf(x[j]), inverse);
         const float stepped = to_step(y[j], bits[j]);
         y[j] = LEAST ? (y[j] > 0.0f ? fmaxf(stepped, 0.001953125f) : y[j]) : copysignf(stepped, x[j]);
     }
@@ -162,8 +162,11 @@ __device__ __forceinline__ float store8_e4m3(uint8_t *p, int left, const float (
     return __uint_as_float(e << 23);
 }
 
+// Four CTAs an SM (64 registers), and as many in the grid: with 74 registers three fit, and the fourth ran alone after them.
+constexpr int kResident = 4;
+
 template <typename G, typename Cp, int BITS>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwArgs a) {
+__global__ void __launch_bounds__(kThreads, kResident) adamw_kernel(const AdamwArgs a) {
     __shared__ float s_rate, s_grow, s_lr;
     pdl_wait();
     const int64_t t = a.counter->step + 1;
@@ -205,8 +208,8 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwArgs a) {
                 const float gj = __fmul_rn(g[j], gs);
                 m[j] = __fadd_rn(__fmul_rn(m[j], a.beta1), __fmul_rn(gj, a.rest1));
                 v[j] = __fadd_rn(__fmul_rn(v[j], a.beta2), __fmul_rn(__fmul_rn(gj, gj), a.rest2));
-                // root and reciprocal are good to 2^-23, on an update that is small against the parameter
-                const float den = __fadd_rn(__fmul_rn(root(v[j]), grow), a.eps);
+                // root and reciprocal are good to 2^-23 (second moments below 2^-126 count as zero here)
+                const float den = __fmaf_rn(root(v[j]), grow, a.eps);
                 p[j] = __fmaf_rn(p[j], keep, -__fmul_rn(rate, __fmul_rn(m[j], reciprocal(den))));
             }
             store8(T.param + at, left, wide, p);
@@ -222,8 +225,8 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwArgs a) {
                 for (int j = 0; j < 8; ++j) {
                     if (j >= left) m[j] = v[j] = 0.0f;
                     const uint32_t h = dither(place + j, key);
-                    lo[j] = h & 0xFFFFu;
-                    hi[j] = h >> 16;
+                    lo[j] = (h << 4) & 0xFFFF0u;
+                    hi[j] = (h >> 12) & 0xFFFF0u;
                 }
                 const float ms = store8_e4m3<false>(reinterpret_cast<uint8_t *>(a.m) + flat, left, m, lo);
                 const float vs = store8_e4m3<true>(reinterpret_cast<uint8_t *>(a.v) + flat, left, v, hi);
@@ -260,7 +263,7 @@ cudaError_t launch_copy(const AdamwArgs &a, int copy, int bits, int grid, cudaSt
 
 cudaError_t launch_adamw(const AdamwArgs &a, int grad_dtype, int copy_dtype, int state_bits, cudaStream_t st) {
     const int64_t chunks = (a.blocks + kAdamwChunk - 1) / kAdamwChunk;
-    int64_t grid = (int64_t)sm_count() * 4;
+    int64_t grid = (int64_t)sm_count() * kResident;
     if (grid > chunks) grid = chunks;
     if (grid < 1) grid = 1;
     return grad_dtype == 2   ? launch_copy<__half>(a, copy_dtype, state_bits, (int)grid, st)

@@ -7,12 +7,12 @@
 // by token first (a stable radix sort), and runs of one token are summed.
 //   1. embed_sort_*: least significant digit first, kDigitBits at a time; a CTA ranks a tile of keys with warp matches and
 //      counters of its own, so equal keys keep their order.  One tile: all digits in one launch.  More: two launches per digit.
-//   2. embed_sum_kernel: a warp takes a window of 32 sorted positions and a strip of columns, loads 16 rows' vectors at a time
-//      and adds them run by run.  A run inside the window is a finished row.  One that crosses its borders leaves a partial
-//      sum: two places a window, in order, so the partial sums are again a sorted list, a sixteenth as long, to which the
-//      same kernel is applied until one window is left.  So a token that occurs once costs one read and one write, one that
+//   2. embed_sum_kernel: a warp takes a window of 32 sorted positions and a strip of columns, loads eight rows' vectors at a
+//      time and adds them run by run.  A run inside the window is a finished row.  One that crosses its borders leaves a
+//      partial sum: two places a window, in order, so the partial sums are again a sorted list, a sixteenth as long, to which
+//      the same is applied until one window is left (by embed_finish_kernel once the list is short).  So a token that occurs once costs one read and one write, one that
 //      fills the batch is summed by as many warps as there are windows, and nothing depends on how frequent tokens are.
-//      The first of these launches also writes zeros to the rows without tokens (a bit per row, set while sorting).
+//      The first of these launches also writes zeros to the rows whose token is not in the list.
 // The grouping of a sum depends on the positions alone.
 #include "train_ops.h"
 
@@ -27,7 +27,6 @@ constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortItems = 4;                // keys a thread ranks at a time
 constexpr int kTile = kSortThreads * kSortItems;
 constexpr int kWindow = 32;
-constexpr int kBatch = 16;                   // rows whose vectors are loaded together
 constexpr int kSumThreads = 256;
 constexpr int kSumWarps = kSumThreads / 32;
 constexpr uint32_t kHole = 0x80000000u;      // a place without a partial sum; its key keeps the list sorted
@@ -107,20 +106,19 @@ __global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a, int group
 // ---- sorting positions by token ---------------------------------------------------------------------------------------
 
 struct SortShared {
-    uint16_t count[kSortWarps][kDigits];   // keys of a digit per warp, then the number before that warp
+    alignas(16) uint16_t count[kSortWarps][kDigits];   // keys of a digit per warp, then the number before that warp
     uint32_t base[kDigits];                // where a digit's keys of this tile go
     uint32_t scan[kSortWarps];
 };
 
-// A position's key: its token, or `rows` (behind all tokens) where it adds nothing.  Sets the token's bit.
-__device__ __forceinline__ uint32_t key_at(const EmbedGradArgs &a, uint32_t *present, int64_t i) {
+// A position's key: its token, or `rows` (behind all tokens) where it adds nothing.
+__device__ __forceinline__ uint32_t key_at(const EmbedGradArgs &a, int64_t i) {
     const int64_t t = token_at(a.tokens, a.token_bits, i);
     if (t == a.padding) return (uint32_t)a.rows;
     if (t < 0 || t >= a.rows) {
         if (a.status) atomicOr(a.status, kStatIndex);
         return (uint32_t)a.rows;
     }
-    if (present) atomicOr(present + (t >> 5), 1u << (t & 31));
     return (uint32_t)t;
 }
 
@@ -128,7 +126,7 @@ __device__ __forceinline__ uint32_t key_at(const EmbedGradArgs &a, uint32_t *pre
 // order is position order.  rank[r]: number of keys of the same digit before this one in the warp; counts per warp in s.count.
 __device__ __forceinline__ void rank_tile(SortShared &s, const uint32_t (&key)[kSortItems], const bool (&have)[kSortItems], int shift,
                                           uint32_t (&rank)[kSortItems]) {
-    for (int d = threadIdx.x; d < kSortWarps * kDigits; d += kSortThreads) (&s.count[0][0])[d] = 0;
+    for (int d = threadIdx.x; d < kSortWarps * kDigits / 8; d += kSortThreads) reinterpret_cast<uint4 *>(&s.count[0][0])[d] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     const int warp = warp_id(), lane = lane_id();
     for (int r = 0; r < kSortItems; ++r) {
@@ -180,13 +178,12 @@ struct SortArgs {
     const uint32_t *in_key, *in_pos;   // the previous digit's order (unused for the first digit)
     uint32_t *out_key, *out_pos;
     uint32_t *counts;                  // [tiles][kDigits]
-    uint32_t *present;                 // a bit per row of the table: some position has its token
     int64_t tiles;
     int shift, digits, first;
 };
 
 __device__ __forceinline__ void load_tile(const SortArgs &s, int64_t tile, uint32_t (&key)[kSortItems], uint32_t (&pos)[kSortItems],
-                                          bool (&have)[kSortItems], bool mark) {
+                                          bool (&have)[kSortItems]) {
     const int64_t at = tile * kTile + (int64_t)warp_id() * (32 * kSortItems) + lane_id();
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
@@ -195,7 +192,7 @@ __device__ __forceinline__ void load_tile(const SortArgs &s, int64_t tile, uint3
         key[r] = 0;
         pos[r] = 0;
         if (have[r]) {
-            key[r] = s.first ? key_at(s.a, mark ? s.present : nullptr, i) : s.in_key[i];
+            key[r] = s.first ? key_at(s.a, i) : s.in_key[i];
             pos[r] = s.first ? (uint32_t)i : s.in_pos[i];
         }
     }
@@ -209,7 +206,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_count_kernel(const So
     __syncthreads();
     uint32_t key[kSortItems], pos[kSortItems];
     bool have[kSortItems];
-    load_tile(s, blockIdx.x, key, pos, have, true);
+    load_tile(s, blockIdx.x, key, pos, have);
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r)
         if (have[r]) atomicAdd(&count[(key[r] >> s.shift) & (kDigits - 1)], 1u);
@@ -223,15 +220,16 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_move_kernel(const Sor
     pdl_wait();
     uint32_t key[kSortItems], pos[kSortItems], rank[kSortItems];
     bool have[kSortItems];
-    load_tile(s, blockIdx.x, key, pos, have, false);
-    rank_tile(sh, key, have, s.shift, rank);
-    warps_before(sh);
+    load_tile(s, blockIdx.x, key, pos, have);
     uint32_t all = 0, mine = 0;
+#pragma unroll 8
     for (int64_t t = 0; t < s.tiles; ++t) {
         const uint32_t c = s.counts[t * kDigits + threadIdx.x];
         if (t < blockIdx.x) mine += c;
         all += c;
     }
+    rank_tile(sh, key, have, s.shift, rank);
+    warps_before(sh);
     sh.base[threadIdx.x] = digits_before(sh, all) + mine;
     __syncthreads();
 #pragma unroll
@@ -249,11 +247,9 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_tile_kernel(const Sor
     __shared__ SortShared sh;
     __shared__ uint32_t keys[kTile], places[kTile];
     pdl_wait();
-    for (int64_t v = threadIdx.x; v < (s.a.rows + 31) / 32; v += kSortThreads) s.present[v] = 0;
-    __syncthreads();
     uint32_t key[kSortItems], pos[kSortItems], rank[kSortItems];
     bool have[kSortItems];
-    load_tile(s, 0, key, pos, have, true);
+    load_tile(s, 0, key, pos, have);
     for (int d = 0; d < s.digits; ++d) {
         const int shift = d * kDigitBits;
         rank_tile(sh, key, have, shift, rank);
@@ -287,26 +283,26 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_tile_kernel(const Sor
         }
 }
 
-__global__ void __launch_bounds__(256) embed_clear_kernel(uint32_t *p, int64_t n) {
-    pdl_wait();
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
-}
-
 // ---- sums ------------------------------------------------------------------------------------------------------------
 
-struct SumArgs {
-    int64_t n;                   // length of the list
-    const uint32_t *key, *pos;   // sorted keys (kHole: nothing there); positions (first list only)
-    const void *from;            // gradient rows, or partial sums by place in the list
+// A sorted list and where its sums go.
+struct List {
+    int64_t n;
+    const uint32_t *key, *pos;   // pos: NULL where rows lie in the list's order
+    const void *from;
     int64_t stride;
-    uint32_t *next_key;          // the list of partial sums, two places a window
+    uint32_t *next_key;          // or NULL
     float *next;
+};
+
+struct SumArgs {
+    List list;                   // sorted keys (kHole: nothing there)
+    float *spare;                // embed_finish_kernel: a place for a third list
     int64_t rows, width;
     float scale;
     int accumulate;
     void *dtable;
-    const uint32_t *present;     // first list, where rows without tokens become zero; else NULL
-    unsigned sum_blocks;
+    unsigned sum_blocks, clear_blocks;   // clear_blocks (first list only): write zeros to the rows without tokens
     int strips;
 };
 
@@ -351,17 +347,41 @@ __device__ __forceinline__ void store_strip(O *row, int64_t strip, int64_t width
     }
 }
 
-// Zeros for the rows of the table without tokens; a warp looks at 32 rows at a time.
+// First place of the sorted list whose key is not below k; the warp together, 32 probes at a time.
+__device__ __forceinline__ int64_t warp_lower_bound(const uint32_t *key, int64_t n, uint32_t k) {
+    int64_t lo = 0, hi = n;
+    while (hi - lo > 0) {
+        const int64_t step = (hi - lo + 31) / 32;
+        const int64_t i = lo + (lane_id() + 1) * step - 1;        // the last place of the lane's part
+        const bool below = i < hi && key[i] < k;
+        const int parts = __popc(__ballot_sync(0xFFFFFFFFu, below));   // parts that lie below k altogether
+        lo += parts * step;
+        hi = min(hi, lo + step - 1);
+        if (step == 1) break;
+    }
+    return lo;
+}
+
+// Zeros for the rows of the table without tokens, 32 rows a warp: the sorted keys say which those are.
 template <typename O, bool WIDE>
 __device__ __forceinline__ void clear_rows(const SumArgs &s, int64_t warp, int64_t warps) {
     O *table = reinterpret_cast<O *>(s.dtable);
-    const int64_t words = (s.rows + 31) / 32;
-    for (int64_t w = warp; w < words; w += warps) {
-        const uint32_t bits = s.present[w];
-        const int rows = (int)min((int64_t)32, s.rows - w * 32);
-        for (int r = 0; r < rows; ++r) {
-            if ((bits >> r) & 1) continue;
-            O *row = table + (w * 32 + r) * s.width;
+    const uint32_t *key = s.list.key;
+    const int64_t n = s.list.n;
+    for (int64_t first = warp * 32; first < s.rows; first += warps * 32) {
+        int64_t lo = warp_lower_bound(key, n, (uint32_t)first);
+        const int64_t end = lo + warp_lower_bound(key + lo, n - lo, (uint32_t)min(first + 32, s.rows));
+        const int64_t mine = first + lane_id();
+        int64_t hi = end;
+        while (lo < hi) {                             // the lane's own row among those
+            const int64_t mid = (lo + hi) / 2;
+            if (key[mid] < (uint32_t)mine) lo = mid + 1;
+            else hi = mid;
+        }
+        const bool empty = mine < s.rows && !(lo < end && key[lo] == (uint32_t)mine);
+        uint32_t rows = __ballot_sync(0xFFFFFFFFu, empty);
+        for (; rows; rows &= rows - 1) {
+            O *row = table + (first + __ffs(rows) - 1) * s.width;
             if constexpr (WIDE) {
                 constexpr int V = 16 / sizeof(O);
                 for (int64_t c = lane_id() * V; c < s.width; c += 32 * V) *reinterpret_cast<uint4 *>(row + c) = make_uint4(0, 0, 0, 0);
@@ -372,89 +392,123 @@ __device__ __forceinline__ void clear_rows(const SumArgs &s, int64_t warp, int64
     }
 }
 
-// T: the list's rows (the gradient's type, or float32 for partial sums); O: the table's.
+// One warp, one window of the list, one strip of columns.  T: the list's rows (the gradient's type, or float32 for partial
+// sums); O: the table's.
 template <typename T, typename O, bool WIDE>
-__global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const SumArgs s) {
+__device__ __forceinline__ void sum_window(const SumArgs &s, const List &l, int64_t w, int64_t strip) {
     constexpr int V = 16 / sizeof(T);
-    pdl_wait();
+    constexpr int kBatch = V == 4 ? 16 : 8;      // rows whose vectors are loaded together
     const int lane = lane_id();
-    if (blockIdx.x >= s.sum_blocks) {
-        clear_rows<O, WIDE>(s, (int64_t)(blockIdx.x - s.sum_blocks) * kSumWarps + warp_id(), (int64_t)(gridDim.x - s.sum_blocks) * kSumWarps);
-        return;
-    }
-    const int64_t windows = (s.n + kWindow - 1) / kWindow, work = windows * s.strips;
-    for (int64_t u = (int64_t)blockIdx.x * kSumWarps + warp_id(); u < work; u += (int64_t)s.sum_blocks * kSumWarps) {
-        const int64_t w = u / s.strips, strip = u - w * s.strips;
-        const int64_t i = w * kWindow + lane;
-        const uint32_t raw = i < s.n ? s.key[i] : 0x7FFFFFFFu;
-        const uint32_t key = raw & ~kHole;
-        const uint32_t pos = s.pos && i < s.n ? s.pos[i] : (uint32_t)i;
-        const uint32_t used = __ballot_sync(0xFFFFFFFFu, raw == key && key < (uint32_t)s.rows);
-        const uint32_t before = w > 0 ? s.key[w * kWindow - 1] & ~kHole : 0x7FFFFFFFu;
-        const uint32_t after = (w + 1) * kWindow < s.n ? s.key[(w + 1) * kWindow] & ~kHole : 0x7FFFFFFFu;
-        const uint32_t next = __shfl_down_sync(0xFFFFFFFFu, key, 1);
-        // where a run ends; the last one of the window may go on
-        const uint32_t ends = __ballot_sync(0xFFFFFFFFu, lane == 31 || next != key);
-        const uint32_t first = __shfl_sync(0xFFFFFFFFu, key, 0), last = __shfl_sync(0xFFFFFFFFu, key, 31);
-        const bool enters = first == before, leaves = last == after;
-        float sum[V] = {};
-        bool any = false, head = true;            // the run holds something; it is the window's first
-        bool full0 = false, full1 = false;        // places of the next list that get a partial sum
+    const int64_t i = w * kWindow + lane;
+    const uint32_t raw = i < l.n ? l.key[i] : 0x7FFFFFFFu;
+    const uint32_t key = raw & ~kHole;
+    const uint32_t pos = l.pos && i < l.n ? l.pos[i] : (uint32_t)i;
+    const uint32_t used = __ballot_sync(0xFFFFFFFFu, raw == key && key < (uint32_t)s.rows);
+    // the keys around the window: its first and its last run may be parts of longer ones
+    const uint32_t before = w > 0 ? l.key[w * kWindow - 1] & ~kHole : 0x7FFFFFFFu;
+    const uint32_t after = (w + 1) * kWindow < l.n ? l.key[(w + 1) * kWindow] & ~kHole : 0x7FFFFFFFu;
+    const uint32_t next = __shfl_down_sync(0xFFFFFFFFu, key, 1);
+    const uint32_t ends = __ballot_sync(0xFFFFFFFFu, lane == 31 || next != key);
+    const uint32_t first = __shfl_sync(0xFFFFFFFFu, key, 0), last = __shfl_sync(0xFFFFFFFFu, key, 31);
+    const bool enters = first == before, leaves = last == after;
+    float sum[V] = {};
+    bool any = false, head = true;            // the run holds something; it is the window's first
+    bool full0 = false, full1 = false;        // places of the next list that get a partial sum
+#pragma unroll 1
+    for (int b = 0; b < kWindow; b += kBatch) {
+        T x[kBatch][V];
 #pragma unroll
-        for (int b = 0; b < kWindow; b += kBatch) {
-            T x[kBatch][V];
+        for (int j = 0; j < kBatch; ++j) {
+            const uint32_t p = __shfl_sync(0xFFFFFFFFu, pos, b + j);
+            if ((used >> (b + j)) & 1) load_strip<T, WIDE, V>(reinterpret_cast<const T *>(l.from) + (int64_t)p * l.stride, strip, s.width, x[j]);
+        }
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-                const uint32_t p = __shfl_sync(0xFFFFFFFFu, pos, b + j);
-                if ((used >> (b + j)) & 1) load_strip<T, WIDE, V>(reinterpret_cast<const T *>(s.from) + (int64_t)p * s.stride, strip, s.width, x[j]);
+        for (int j = 0; j < kBatch; ++j) {
+            if ((used >> (b + j)) & 1) {
+                any = true;
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] = __fadd_rn(sum[e], Conv<T>::up(x[j][e]));
             }
+            if ((ends >> (b + j)) & 1) {
+                const bool tail = b + j == 31 && leaves, from_before = head && enters;
+                if (any) {
+                    if (tail || from_before) {
+                        full0 |= from_before;
+                        full1 |= !from_before;
+                        store_strip<float, WIDE, V>(l.next + (2 * w + (from_before ? 0 : 1)) * s.width, strip, s.width, sum);
+                    } else {
+                        const uint32_t row = __shfl_sync(0xFFFFFFFFu, key, b + j);
+                        O *out = reinterpret_cast<O *>(s.dtable) + (int64_t)row * s.width;
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-                if ((used >> (b + j)) & 1) {
-                    any = true;
+                        for (int e = 0; e < V; ++e) sum[e] = __fmul_rn(sum[e], s.scale);
+                        if (s.accumulate) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) sum[e] = __fadd_rn(sum[e], Conv<T>::up(x[j][e]));
-                }
-                if ((ends >> (b + j)) & 1) {
-                    const bool tail = b + j == 31 && leaves, from_before = head && enters;
-                    if (any) {
-                        if (tail || from_before) {
-                            const int at = from_before ? 0 : 1;
-                            full0 |= from_before;
-                            full1 |= !from_before;
-                            store_strip<float, WIDE, V>(s.next + (2 * w + at) * s.width, strip, s.width, sum);
-                        } else {
-                            const uint32_t row = __shfl_sync(0xFFFFFFFFu, key, b + j);
-                            O *out = reinterpret_cast<O *>(s.dtable) + (int64_t)row * s.width;
-#pragma unroll
-                            for (int e = 0; e < V; ++e) sum[e] = __fmul_rn(sum[e], s.scale);
-                            if (s.accumulate) {
-#pragma unroll
-                                for (int e = 0; e < V; ++e) {
-                                    const int64_t c = column<WIDE, V>(strip, e);
-                                    if (c < s.width) sum[e] = __fadd_rn(Conv<O>::up(out[c]), sum[e]);
-                                }
+                            for (int e = 0; e < V; ++e) {
+                                const int64_t c = column<WIDE, V>(strip, e);
+                                if (c < s.width) sum[e] = __fadd_rn(Conv<O>::up(out[c]), sum[e]);
                             }
-                            store_strip<O, WIDE, V>(out, strip, s.width, sum);
                         }
+                        store_strip<O, WIDE, V>(out, strip, s.width, sum);
                     }
-#pragma unroll
-                    for (int e = 0; e < V; ++e) sum[e] = 0.0f;
-                    any = head = false;
                 }
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] = 0.0f;
+                any = head = false;
             }
         }
-        if (strip == 0 && lane < 2 && s.next_key) s.next_key[2 * w + lane] = (lane == 0 ? first : last) | ((lane == 0 ? full0 : full1) ? 0u : kHole);
+    }
+    if (lane < 2 && l.next_key) l.next_key[2 * w + lane] = (lane == 0 ? first : last) | ((lane == 0 ? full0 : full1) ? 0u : kHole);
+}
+
+template <typename T, typename O, bool WIDE>
+__global__ void __launch_bounds__(kSumThreads, sizeof(T) == 4 ? 2 : 3) embed_sum_kernel(const SumArgs s) {
+    pdl_wait();
+    // the clearing CTAs lie evenly among the others, so that reading and writing go on side by side
+    const int64_t all = gridDim.x, b = blockIdx.x;
+    const int64_t cleared = b * s.clear_blocks / all;
+    if ((b + 1) * s.clear_blocks / all > cleared) {
+        clear_rows<O, WIDE>(s, cleared * kSumWarps + warp_id(), (int64_t)s.clear_blocks * kSumWarps);
+        return;
+    }
+    const int64_t work = (s.list.n + kWindow - 1) / kWindow * s.strips;
+    for (int64_t u = (b - cleared) * kSumWarps + warp_id(); u < work; u += (int64_t)s.sum_blocks * kSumWarps) {
+        const int64_t w = u / s.strips, strip = u - w * s.strips;
+        List l = s.list;
+        if (strip != 0) l.next_key = nullptr;     // (every strip finds the same)
+        sum_window<T, O, WIDE>(s, l, w, strip);
+    }
+}
+
+// The last lists of partial sums, a CTA per strip: it keeps the keys of the lists that it makes to itself.
+constexpr int kFinish = 512;
+template <typename O, bool WIDE>
+__global__ void __launch_bounds__(kSumThreads, 2) embed_finish_kernel(const SumArgs s) {
+    __shared__ uint32_t keys[2][2 * kFinish / kWindow];
+    pdl_wait();
+    List l = s.list;
+    float *spare = s.spare;
+    for (int level = 0;; ++level) {
+        const int64_t windows = (l.n + kWindow - 1) / kWindow;
+        l.next_key = windows > 1 ? keys[level & 1] : nullptr;
+        for (int64_t w = warp_id(); w < windows; w += kSumWarps) sum_window<float, O, WIDE>(s, l, w, blockIdx.x);
+        if (windows <= 1) return;
+        __syncthreads();
+        l.n = 2 * windows;
+        l.key = l.next_key;
+        float *was = (float *)l.from;
+        l.from = l.next;
+        l.next = level == 0 ? spare : was;
     }
 }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct GradLayout {
-    size_t key[2], pos[2], counts, present, next_key[2], next[2], total;
+    size_t key[2], pos[2], counts, next_key[3], next[3], total;
     int64_t tiles;
 };
-inline int64_t next_length(int64_t n) { return 2 * ((n + kWindow - 1) / kWindow); }
+// Places of the list that a list of n leaves (0: none).
+inline int64_t next_length(int64_t n) { return n > kWindow ? 2 * ((n + kWindow - 1) / kWindow) : 0; }
 GradLayout grad_layout(int64_t n, int64_t rows, int64_t width) {
     GradLayout L{};
     size_t off = 0;
@@ -464,29 +518,29 @@ GradLayout grad_layout(int64_t n, int64_t rows, int64_t width) {
         L.pos[i] = off, off = up256(off + (size_t)n * 4);
     }
     L.counts = off, off = up256(off + (size_t)L.tiles * kDigits * 4);
-    L.present = off, off = up256(off + (size_t)((rows + 31) / 32) * 4);
-    // two lists of partial sums, used in turn
-    int64_t m = n > kWindow ? next_length(n) : 0;
-    for (int i = 0; i < 2; ++i) {
+    // lists of partial sums: each is read while the next one is written
+    int64_t m = next_length(n);
+    for (int i = 0; i < 3; ++i) {
         L.next_key[i] = off, off = up256(off + (size_t)m * 4);
         L.next[i] = off, off = up256(off + (size_t)m * width * 4);
-        m = m > kWindow ? next_length(m) : 0;
+        m = next_length(m);
     }
     L.total = off ? off : 256;
     return L;
 }
 
 template <typename T, typename O>
-cudaError_t launch_sum(SumArgs s, bool wide, cudaStream_t st) {
+cudaError_t launch_sum(SumArgs s, bool first, bool wide, cudaStream_t st) {
     const int64_t most = (int64_t)sm_count() * 8;
     constexpr int V = 16 / sizeof(T);
     s.strips = (int)((s.width + 32 * V - 1) / (32 * V));
-    const int64_t work = (s.n + kWindow - 1) / kWindow * s.strips;
+    const int64_t work = (s.list.n + kWindow - 1) / kWindow * s.strips;
     int64_t blocks = (work + kSumWarps - 1) / kSumWarps;
     if (blocks > most * 16) blocks = most * 16;
     s.sum_blocks = (unsigned)blocks;
-    int64_t clear = s.present ? (s.rows + 32 * kSumWarps - 1) / (32 * kSumWarps) : 0;
-    if (clear > most) clear = most;
+    int64_t clear = first && !s.accumulate ? (s.rows + 32 * kSumWarps - 1) / (32 * kSumWarps) : 0;
+    if (clear > most * 4) clear = most * 4;
+    s.clear_blocks = (unsigned)clear;
     if (blocks + clear == 0) return cudaSuccess;
     const dim3 grid((unsigned)(blocks + clear)), block(kSumThreads);
     return wide ? launch_after(embed_sum_kernel<T, O, true>, grid, block, st, s) : launch_after(embed_sum_kernel<T, O, false>, grid, block, st, s);
@@ -496,18 +550,19 @@ cudaError_t launch_sum(SumArgs s, bool wide, cudaStream_t st) {
 template <typename T>
 cudaError_t launch_sums(SumArgs s, const GradLayout &L, char *ws, bool wide, cudaStream_t st) {
     for (int level = 0;; ++level) {
-        const bool last = s.n <= kWindow;
-        const int to = level & 1;
-        s.next_key = last ? nullptr : (uint32_t *)(ws + L.next_key[to]);
-        s.next = last ? nullptr : (float *)(ws + L.next[to]);
-        const cudaError_t e = level == 0 ? launch_sum<T, T>(s, wide, st) : launch_sum<float, T>(s, wide, st);
-        if (e != cudaSuccess || last) return e;
-        s.n = next_length(s.n);
-        s.key = s.next_key;
-        s.from = s.next;
-        s.pos = nullptr;
-        s.stride = s.width;
-        s.present = nullptr;
+        const int to = level % 3;       // three lists in turn: the first two lengths are the largest
+        const int64_t next = next_length(s.list.n);
+        s.list.next_key = next ? (uint32_t *)(ws + L.next_key[to]) : nullptr;
+        s.list.next = next ? (float *)(ws + L.next[to]) : nullptr;
+        cudaError_t e;
+        if (level > 0 && s.list.n <= kFinish) {
+            s.spare = (float *)(ws + L.next[(to + 1) % 3]);
+            const dim3 grid((unsigned)((s.width + 127) / 128)), block(kSumThreads);
+            return wide ? launch_after(embed_finish_kernel<T, true>, grid, block, st, s) : launch_after(embed_finish_kernel<T, false>, grid, block, st, s);
+        }
+        e = level == 0 ? launch_sum<T, T>(s, true, wide, st) : launch_sum<float, T>(s, false, wide, st);
+        if (e != cudaSuccess || !next) return e;
+        s.list = List{next, s.list.next_key, nullptr, s.list.next, s.width, nullptr, nullptr};
     }
 }
 
@@ -535,7 +590,6 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
     SortArgs s{};
     s.a = a;
     s.counts = (uint32_t *)(ws + L.counts);
-    s.present = (uint32_t *)(ws + L.present);
     s.tiles = L.tiles;
     int bits = 1;
     while (bits < 32 && (a.rows >> bits) != 0) ++bits;      // keys 0 .. rows
@@ -549,9 +603,6 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
         e = launch_after(embed_sort_tile_kernel, dim3(1), dim3(kSortThreads), st, s);
         if (e != cudaSuccess) return e;
     } else {
-        const int64_t words = (a.rows + 31) / 32, blocks = (words + 255) / 256;
-        e = launch_after(embed_clear_kernel, dim3((unsigned)(blocks < sm_count() ? blocks : sm_count())), dim3(256), st, s.present, words);
-        if (e != cudaSuccess) return e;
         for (int d = 0; d < s.digits; ++d) {
             s.first = d == 0;
             s.shift = d * kDigitBits;
@@ -567,17 +618,12 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
         }
     }
     SumArgs u{};
-    u.n = a.n;
-    u.key = (const uint32_t *)(ws + L.key[at]);
-    u.pos = (const uint32_t *)(ws + L.pos[at]);
-    u.from = a.grad;
-    u.stride = a.stride;
+    u.list = List{a.n, (const uint32_t *)(ws + L.key[at]), (const uint32_t *)(ws + L.pos[at]), a.grad, a.stride, nullptr, nullptr};
     u.rows = a.rows;
     u.width = a.width;
     u.scale = a.scale;
     u.accumulate = a.accumulate;
     u.dtable = a.dtable;
-    u.present = a.accumulate ? nullptr : s.present;
     const size_t b = dtype_bytes(dtype);
     const bool wide = aligned(a.grad, 16) && aligned(a.dtable, 16) && (a.width * b) % 16 == 0 && (a.stride * b) % 16 == 0;
     return dtype == 0   ? launch_sums<float>(u, L, ws, wide, st)
