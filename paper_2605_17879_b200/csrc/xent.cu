@@ -3,8 +3,10 @@
 //   z = x w^T;  lse_n = log sum_v exp z_nv;  loss_n = lse_n - z_n,target(n)
 //   G_nv = g_n (exp(z_nv - lse_n) - [v = target(n)]);  dx = G w;  dw = G^T x
 //
-// All four products run on the tensor cores in one kernel frame (product_kernel): a warp loads tiles by TMA, one thread issues
-// tcgen05.mma into TMEM, eight warps read the finished accumulator while the next one is filled.  What differs is the last
+// All four products run on the tensor cores in one kernel frame (product_kernel): pairs of CTAs take tiles of 256 x 256, each
+// CTA loads its half of either operand by TMA, one thread issues tcgen05.mma into the TMEM of both, and eight warps a CTA
+// read the finished accumulator while the next one is filled.  Single CTAs with tiles of 128 x 256 load half as much again
+// per product and were bound by that (50 bytes a cycle and SM).  What differs is the last
 // step on an accumulator: the logits' largest value and sum of exponentials per row (the forward pass), G in 16 bits (the
 // backward pass computes the logits again, a piece of the vocabulary at a time), or a gradient.
 //
@@ -29,12 +31,15 @@ namespace guard {
 
 namespace {
 
-constexpr int kM = 128, kN = 256, kK = 64;    // a tile: rows, columns, depth of a stage
-constexpr int kStages = 4;
-constexpr int kABytes = kM * kK * 2, kBBytes = kN * kK * 2;
+constexpr int kM = 256, kN = 256, kK = 64;    // a tile: rows, columns, depth of a stage
+constexpr int kHalf = 128;                    // rows of either operand that each CTA of the pair holds
+constexpr int kStages = 6;
+constexpr int kOperand = kHalf * kK * 2;      // bytes
+constexpr int kStage = 2 * kOperand;
+constexpr int kPass = 1024 / kK;              // stages that one accumulator takes in the forward pass
 constexpr int kEpilogueWarps = 8;
 constexpr int kProductThreads = 32 * (4 + kEpilogueWarps);
-constexpr int kProductSmem = kStages * (kABytes + kBBytes) + 1024;
+constexpr int kProductSmem = kStages * kStage + 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 
 enum Mode { kStats, kGrad, kDx, kDw };
@@ -143,14 +148,37 @@ __device__ __forceinline__ void store_row32(T *p, int left, bool wide, const flo
         if (j < left) p[j] = Conv<T>::down(x[j]);
 }
 
-template <int MODE, typename T>
-__global__ void __launch_bounds__(kProductThreads, 1)
+// What a thread of the forward pass knows of its row: largest value so far, and the sum of exponentials relative to it.
+struct RowSum {
+    float top, sum;
+    __device__ __forceinline__ void add(const float (&z)[32]) {
+        float most = top;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) most = fmaxf(most, z[j]);
+        const float base = finite_or_zero(most);
+        const float shift = -__fmul_rn(base, kLog2e);
+        if (sum != 0.0f) sum = __fmul_rn(sum, exp2_fast(__fmul_rn(__fsub_rn(finite_or_zero(top), base), kLog2e)));
+        float part[4] = {};
+#pragma unroll
+        for (int j = 0; j < 32; ++j) part[j & 3] = __fadd_rn(part[j & 3], exp2_fast(__fmaf_rn(z[j], kLog2e, shift)));
+        sum = __fadd_rn(sum, __fadd_rn(__fadd_rn(part[0], part[1]), __fadd_rn(part[2], part[3])));
+        top = most;
+    }
+};
+
+// LONG: the depth takes more than one pass.  The tensor cores cut off what an accumulator's last bit cannot hold, product
+// step by product step, which shrinks a logit by some 2^-24 a step; the forward pass, whose results are float32, starts a new
+// accumulator every kPass stages and adds them in registers, rounded to nearest (loss of 4 096 deep logits off by 6e-7
+// of itself instead of 1.2e-6).
+template <int MODE, bool LONG, typename T>
+__global__ void __launch_bounds__(kProductThreads, 1) __cluster_dims__(2, 1, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a2, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ CUtensorMap map_b2, const ProductArgs a) {
     extern __shared__ uint8_t raw[];
     __shared__ ProductShared s;
     uint8_t *tiles = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     const int warp = warp_id(), lane = lane_id();
+    const uint32_t rank = cluster_rank();
     pdl_wait();
 
     const int rows = a.head ? a.head->count : a.rows;
@@ -159,6 +187,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     if (MODE == kDw) k_blocks = (rows + kK - 1) / kK;
     else m_tiles = (rows + kM - 1) / kM;
     const int total = m_tiles * a.n_tiles * a.splits;
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int pass = LONG ? kPass : k_blocks + 1;      // stages an accumulator takes
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
@@ -167,19 +197,19 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.done[i], 1);
-            mbar_init(&s.free_[i], kEpilogueWarps);
+            mbar_init(&s.free_[i], 2 * kEpilogueWarps);
         }
         mbar_init(&s.drain, 1);
         s.abort = 0;
     }
     if (warp == 2) tmem_alloc(&s.tmem, 512);
     tc_fence_before();
-    __syncthreads();
+    cluster_sync();
     tc_fence_after();
     const uint32_t tmem = s.tmem;
 
     if (warp == 0 && lane == 0) {
-        // ---- loads
+        // ---- loads: this CTA's half of the rows of either operand
         // the rows' operand: x, which is read where it is when every row takes part (A of the logits, B of dw)
         const CUtensorMap *pa = MODE == kStats || MODE == kGrad ? (whole ? &map_a : &map_a2) : &map_a;
         const CUtensorMap *pb = MODE == kDw ? (whole ? &map_b : &map_b2) : &map_b;
@@ -187,62 +217,72 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         tma_prefetch_map(pb);
         uint32_t it = 0;
         bool ok = true;
-        for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
+        for (int t = pair; t < total && ok; t += pairs) {
             const Tile tl = tile_at(t, m_tiles, a.n_tiles, a.group, a.splits);
             const int k0 = (int)((int64_t)k_blocks * tl.split / a.splits), k1 = (int)((int64_t)k_blocks * (tl.split + 1) / a.splits);
+            const int m0 = tl.m * kM + rank * kHalf, n0 = tl.n * kN + rank * kHalf;
             for (int k = k0; k < k1; ++k, ++it) {
                 const int st = it % kStages;
                 if (!(ok = wait_for(s, &s.empty[st], ((it / kStages) & 1) ^ 1))) break;
-                uint8_t *sa = tiles + st * (kABytes + kBBytes), *sb = sa + kABytes;
-                mbar_arrive_expect_tx(&s.full[st], kABytes + kBBytes);
+                uint8_t *sa = tiles + st * kStage, *sb = sa + kOperand;
+                const uint32_t full = in_first(&s.full[st]);
+                if (rank == 0) mbar_arrive_expect_tx(&s.full[st], 2 * kStage);      // of both CTAs
                 if (MODE == kDw) {          // A: G, tokens by vocabulary; the vocabulary (rows of dw) is contiguous
-                    for (int h = 0; h < kM / 64; ++h) tma_load(sa + h * 8192, pa, tl.m * kM + h * 64, k * kK, &s.full[st]);
+                    for (int h = 0; h < kHalf / 64; ++h) tma_load(sa + h * 8192, pa, m0 + h * 64, k * kK, full);
                 } else {
-                    tma_load(sa, pa, k * kK, tl.m * kM, &s.full[st]);
+                    tma_load(sa, pa, k * kK, m0, full);
                 }
                 if (MODE == kStats || MODE == kGrad) {
-                    tma_load(sb, pb, k * kK, (int)a.v0 + tl.n * kN, &s.full[st]);
+                    tma_load(sb, pb, k * kK, (int)a.v0 + n0, full);
                 } else {                    // B: w or x, whose columns (of the result) are contiguous
                     const int y = MODE == kDx ? (int)a.v0 + k * kK : k * kK;
-                    for (int h = 0; h < kN / 64; ++h) tma_load(sb + h * 8192, pb, tl.n * kN + h * 64, y, &s.full[st]);
+                    for (int h = 0; h < kHalf / 64; ++h) tma_load(sb + h * 8192, pb, n0 + h * 64, y, full);
                 }
             }
         }
-        if (*(volatile uint32_t *)&s.abort) {       // given up: let the copies in flight land before the memory is anyone else's
+        if (rank == 0 && *(volatile uint32_t *)&s.abort) {       // given up: let the copies in flight land before the memory is anyone else's
             for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) {
                 const long long t0 = clock64();
                 while (!mbar_try_wait(&s.full[i % kStages], (i / kStages) & 1) && clock64() - t0 < kWaitLimitCycles) {}
             }
         }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1 && lane == 0 && rank == 0) {
         // ---- products
-        constexpr uint32_t type = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+        constexpr uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
         constexpr uint32_t a_rows_contiguous = MODE == kDw, b_rows_contiguous = MODE == kDx || MODE == kDw;
         constexpr uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | (a_rows_contiguous << 15) | (b_rows_contiguous << 16) |
                                    ((kN / 8) << 17) | ((kM / 16) << 24);
         uint32_t it = 0, nth = 0;
         bool ok = true;
-        for (int t = blockIdx.x; t < total && ok; t += gridDim.x, ++nth) {
+        for (int t = pair; t < total && ok; t += pairs) {
             const int split = t % a.splits;
             const int k0 = (int)((int64_t)k_blocks * split / a.splits), k1 = (int)((int64_t)k_blocks * (split + 1) / a.splits);
-            const uint32_t acc = nth & 1;
-            if (!(ok = wait_for(s, &s.free_[acc], ((nth >> 1) & 1) ^ 1))) break;
-            tc_fence_after();
-            for (int k = k0; k < k1; ++k, ++it) {
-                const int st = it % kStages;
-                if (!(ok = wait_for(s, &s.full[st], (it / kStages) & 1))) break;
+            for (int p0 = k0; ok; p0 += pass, ++nth) {          // (once even where there is no depth)
+                const uint32_t acc = nth & 1;
+                const int p1 = min(k1, p0 + pass);
+                if (!(ok = wait_for(s, &s.free_[acc], ((nth >> 1) & 1) ^ 1))) break;
                 tc_fence_after();
-                const uint8_t *sa = tiles + st * (kABytes + kBBytes), *sb = sa + kABytes;
+                for (int k = p0; k < p1; ++k, ++it) {
+                    const int st = it % kStages;
+                    if (!(ok = wait_for(s, &s.full[st], (it / kStages) & 1))) break;
+                    tc_fence_after();
+                    const uint8_t *sa = tiles + st * kStage, *sb = sa + kOperand;
 #pragma unroll
-                for (int j = 0; j < kK / 16; ++j) {
-                    // depth contiguous: 16 elements on in a row of 128 bytes; rows contiguous: 16 rows of 128 bytes on
-                    const uint64_t da = smem_desc(sa + (a_rows_contiguous ? j * 2048 : j * 32), 8192, 1024);
-                    const uint64_t db = smem_desc(sb + (b_rows_contiguous ? j * 2048 : j * 32), 8192, 1024);
-                    tc_mma(tmem + acc * kN, da, db, idesc, k > k0 || j > 0);
+                    for (int j = 0; j < kK / 16; ++j) {
+                        // depth contiguous: 16 elements on in a row of 128 bytes; rows contiguous: 16 rows of 128 bytes on
+                        const uint64_t da = smem_desc(sa + (a_rows_contiguous ? j * 2048 : j * 32), 8192, 1024);
+                        const uint64_t db = smem_desc(sb + (b_rows_contiguous ? j * 2048 : j * 32), 8192, 1024);
+                        tc_mma(tmem + acc * kN, da, db, idesc, k > p0 || j > 0);
+                    }
+                    tc_commit(&s.empty[st]);
                 }
-                tc_commit(&s.empty[st]);
+                if (!ok) break;
+                tc_commit(&s.done[acc]);
+                if (p1 >= k1) {
+                    ++nth;
+                    break;
+                }
             }
-            if (ok) tc_commit(&s.done[acc]);
         }
         if (*(volatile uint32_t *)&s.abort) {
             tc_commit(&s.drain);
@@ -252,13 +292,13 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     } else if (warp >= 4) {
         // ---- what becomes of an accumulator: a thread has a row, and half of its columns
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const uint32_t mine = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
         const float inverse = a.head ? a.head->inverse : 1.0f;
+        const uint32_t free0 = in_first(&s.free_[0]), free1 = in_first(&s.free_[1]);
         uint32_t nth = 0;
-        for (int t = blockIdx.x; t < total; t += gridDim.x, ++nth) {
+        for (int t = pair; t < total; t += pairs) {
             const Tile tl = tile_at(t, m_tiles, a.n_tiles, a.group, a.splits);
-            const uint32_t acc = nth & 1;
-            const int row = tl.m * kM + quarter * 32 + lane;
+            const int row = tl.m * kM + rank * kHalf + quarter * 32 + lane;
             bool empty = false;       // no depth at all: the accumulator was not written
             if (MODE == kDw || MODE == kDx)
                 empty = (int)((int64_t)k_blocks * tl.split / a.splits) == (int)((int64_t)k_blocks * (tl.split + 1) / a.splits);
@@ -274,19 +314,44 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     }
                 }
             }
-            if (!__all_sync(0xFFFFFFFFu, wait_for(s, &s.done[acc], (nth >> 1) & 1))) break;   // (the warp stays together)
+            float held[LONG ? 128 : 1];
+            bool ok = true;
+            if constexpr (LONG) {     // all passes but the last are added up in registers
+                for (int p = 0; p + kPass < k_blocks; p += kPass, ++nth) {
+                    const uint32_t acc = nth & 1;
+                    ok = __all_sync(0xFFFFFFFFu, wait_for(s, &s.done[acc], (nth >> 1) & 1));   // (the warp stays together)
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t r[16];
+                        tmem_load16(mine + acc * kN + c * 16, r);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) held[c * 16 + j] = p == 0 ? __uint_as_float(r[j]) : __fadd_rn(held[c * 16 + j], __uint_as_float(r[j]));
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_at(acc ? free1 : free0);
+                }
+                if (!ok) break;
+            }
+            const uint32_t acc = nth & 1;
+            if (!__all_sync(0xFFFFFFFFu, wait_for(s, &s.done[acc], (nth >> 1) & 1))) break;
+            ++nth;
             tc_fence_after();
-            float top = -INFINITY, sum = 0.0f;
-#pragma unroll 1
+            RowSum sums{-INFINITY, 0.0f};
+            constexpr int kUnroll = LONG ? 4 : 1;
+#pragma unroll kUnroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t r[32];
                 float x[32];
-                tmem_load32(tmem + lanes + acc * kN + half * 128 + c * 32, r);
+                tmem_load32(mine + acc * kN + c * 32, r);
                 tmem_load_wait();
                 if (c == 3) {         // the accumulator is free once every warp has read its part
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&s.free_[acc]);
+                    if (lane == 0) mbar_arrive_at(acc ? free1 : free0);
                 }
                 const int64_t col = (int64_t)tl.n * kN + half * 128 + c * 32;
                 if (MODE == kStats || MODE == kGrad) {
@@ -295,29 +360,24 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     const bool here = at >= 0 && at < 32;
                     const int left = (int)min((int64_t)32, max((int64_t)0, a.vocab - first));
                     if (MODE == kStats) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            x[j] = __uint_as_float(r[j]);
+                            if constexpr (LONG) x[j] = __fadd_rn(held[c * 32 + j], x[j]);
+                        }
                         if (left < 32) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j)
-                                if (j >= left) r[j] = 0xFF800000u;
+                                if (j >= left) x[j] = -INFINITY;
                         }
                         if (__any_sync(0xFFFFFFFFu, here)) {
                             float z = 0.0f;
 #pragma unroll
                             for (int j = 0; j < 32; ++j)
-                                if (j == (int)at) z = __uint_as_float(r[j]);
+                                if (j == (int)at) z = x[j];
                             if (here) a.picked[row] = z;
                         }
-                        float most = top;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) most = fmaxf(most, __uint_as_float(r[j]));
-                        const float base = finite_or_zero(most);
-                        const float shift = -__fmul_rn(base, kLog2e);
-                        if (sum != 0.0f) sum = __fmul_rn(sum, exp2_fast(__fmul_rn(__fsub_rn(finite_or_zero(top), base), kLog2e)));
-                        float part[4] = {};
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) part[j & 3] = __fadd_rn(part[j & 3], exp2_fast(__fmaf_rn(__uint_as_float(r[j]), kLog2e, shift)));
-                        sum = __fadd_rn(sum, __fadd_rn(__fadd_rn(part[0], part[1]), __fadd_rn(part[2], part[3])));
-                        top = most;
+                        sums.add(x);
                     } else {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) {
@@ -357,11 +417,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     }
                 }
             }
-            if (MODE == kStats && row < rows) a.parts[(int64_t)row * a.n_parts + tl.n * 2 + half] = make_float2(top, sum);
+            if (MODE == kStats && row < rows) a.parts[(int64_t)row * a.n_parts + tl.n * 2 + half] = make_float2(sums.top, sums.sum);
         }
     }
     tc_fence_before();
-    __syncthreads();
+    __syncwarp();
+    cluster_sync();              // the pair's memory and barriers are used by both until here
     tc_fence_after();
     if (threadIdx.x == 0 && s.abort && a.status) atomicOr(a.status, kStatTimeout);
     if (warp == 2) tmem_free(tmem, 512);
@@ -614,7 +675,7 @@ bool make_map(CUtensorMap *map, bool bf16, const void *p, int64_t width, int64_t
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr int kDirectRows = kM;       // up to here the forward pass takes the rows as they are: there is no tile to save
+constexpr int kDirectRows = kHalf;     // up to here the forward pass takes the rows as they are: there is no tile to save
 
 struct XentLayout {
     size_t head, target, row_of, place, lse, grad, picked, parts, x, g, partial, total;
@@ -650,7 +711,7 @@ XentLayout layout(int64_t rows, int64_t width, int64_t vocab, bool grads) {
         L.piece = piece;
         take(L.g, (size_t)L.padded * piece * 2);
         const int64_t tiles = L.padded / kM * ((width + kN - 1) / kN);
-        int64_t splits = sm_count() / tiles;
+        int64_t splits = sm_count() / 2 / tiles;
         const int64_t depth = piece / kK;
         if (splits > depth / 4) splits = depth / 4;
         if (splits < 1) splits = 1;
@@ -662,13 +723,19 @@ XentLayout layout(int64_t rows, int64_t width, int64_t vocab, bool grads) {
     return L;
 }
 
-template <int MODE, typename T>
-cudaError_t launch_product(const CUtensorMap &ma, const CUtensorMap &ma2, const CUtensorMap &mb, const CUtensorMap &mb2, const ProductArgs &a, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(product_kernel<MODE, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
+template <int MODE, bool LONG, typename T>
+cudaError_t launch_product_as(const CUtensorMap &ma, const CUtensorMap &ma2, const CUtensorMap &mb, const CUtensorMap &mb2, const ProductArgs &a, cudaStream_t st) {
+    cudaError_t e = cudaFuncSetAttribute(product_kernel<MODE, LONG, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
     if (e != cudaSuccess) return e;
     const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * a.splits;
-    const int64_t sms = sm_count();
-    return launch_after_smem(product_kernel<MODE, T>, dim3((unsigned)(tiles < sms ? tiles : sms)), dim3(kProductThreads), kProductSmem, st, ma, ma2, mb, mb2, a);
+    const int64_t pairs = sm_count() / 2;
+    return launch_after_smem(product_kernel<MODE, LONG, T>, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), dim3(kProductThreads), kProductSmem, st, ma, ma2, mb, mb2, a);
+}
+template <int MODE, typename T>
+cudaError_t launch_product(const CUtensorMap &ma, const CUtensorMap &ma2, const CUtensorMap &mb, const CUtensorMap &mb2, const ProductArgs &a, cudaStream_t st) {
+    if constexpr (MODE == kStats)
+        if (a.k_blocks > kPass) return launch_product_as<MODE, true, T>(ma, ma2, mb, mb2, a, st);
+    return launch_product_as<MODE, false, T>(ma, ma2, mb, mb2, a, st);
 }
 
 // Row tiles that share a column tile: as many as fit in about a third of the second-level cache.
@@ -728,10 +795,10 @@ cudaError_t forward(const XentArgs &x, cudaStream_t st) {
     const bool direct = x.rows <= kDirectRows, bf16 = x.dtype == 1;
     cudaError_t e;
     CUtensorMap mx, mg, mw;
-    if (!make_map(&mx, bf16, x.x, x.width, x.rows, x.x_stride, kM) || !make_map(&mw, bf16, x.w, x.width, x.vocab, x.w_stride, kN)) return cudaErrorInvalidValue;
+    if (!make_map(&mx, bf16, x.x, x.width, x.rows, x.x_stride, kHalf) || !make_map(&mw, bf16, x.w, x.width, x.vocab, x.w_stride, kHalf)) return cudaErrorInvalidValue;
     mg = mx;
     if (!direct) {
-        if (!make_map(&mg, bf16, ws + L.x, x.width, L.padded, x.width, kM)) return cudaErrorInvalidValue;
+        if (!make_map(&mg, bf16, ws + L.x, x.width, L.padded, x.width, kHalf)) return cudaErrorInvalidValue;
         e = launch_rows(x, L, false, st);
         if (e != cudaSuccess) return e;
     }
@@ -782,8 +849,8 @@ cudaError_t backward(const XentArgs &x, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     CUtensorMap mx, mxg, mw, gk, gm, wn, xn, xng;
     // G as the rows' operand of dx (its vocabulary is the depth) and of dw (its vocabulary are the rows)
-    if (!make_map(&mx, bf16, x.x, x.width, x.rows, x.x_stride, kM) || !make_map(&mxg, bf16, ws + L.x, x.width, L.padded, x.width, kM) ||
-        !make_map(&mw, bf16, x.w, x.width, x.vocab, x.w_stride, kN) || !make_map(&gk, bf16, ws + L.g, L.piece, L.padded, L.piece, kM) ||
+    if (!make_map(&mx, bf16, x.x, x.width, x.rows, x.x_stride, kHalf) || !make_map(&mxg, bf16, ws + L.x, x.width, L.padded, x.width, kHalf) ||
+        !make_map(&mw, bf16, x.w, x.width, x.vocab, x.w_stride, kHalf) || !make_map(&gk, bf16, ws + L.g, L.piece, L.padded, L.piece, kHalf) ||
         !make_map(&gm, bf16, ws + L.g, L.piece, L.padded, L.piece, kK) || !make_map(&wn, bf16, x.w, x.width, x.vocab, x.w_stride, kK) ||
         !make_map(&xn, bf16, x.x, x.width, x.rows, x.x_stride, kK) || !make_map(&xng, bf16, ws + L.x, x.width, L.padded, x.width, kK))
         return cudaErrorInvalidValue;
@@ -819,7 +886,7 @@ cudaError_t backward(const XentArgs &x, cudaStream_t st) {
             d.n_tiles = width_tiles;
             d.k_blocks = (int)((here + kK - 1) / kK);
             d.splits = L.splits;
-            d.group = row_tiles < 16 ? row_tiles : 16;
+            d.group = row_tiles < 8 ? row_tiles : 8;
             d.out = x.dx;
             d.out_stride = x.width;
             d.partial = direct ? nullptr : (float *)(ws + L.partial);
@@ -833,7 +900,7 @@ cudaError_t backward(const XentArgs &x, cudaStream_t st) {
             d.m_tiles = (int)((here + kM - 1) / kM);
             d.n_tiles = width_tiles;
             d.splits = 1;
-            d.group = d.m_tiles < 16 ? d.m_tiles : 16;
+            d.group = d.m_tiles < 8 ? d.m_tiles : 8;
             d.out = x.dw;
             d.out_stride = x.width;
             e = launch_product<kDw, T>(gm, gm, xn, xng, d, st);
