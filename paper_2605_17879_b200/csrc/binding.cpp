@@ -1,9 +1,11 @@
 // Python marshalling of the calls a monitor makes every step: checks the tensors, takes their device pointers and the
 // current stream, and calls the C ABI with the GIL released.  The same checks written in Python cost more than the
 // kernels of a small fleet: ten output tensors, five attributes each, a stream object and a foreign call are some 15 us
-// per evaluation, against under 2 us here.
+// per evaluation, against under 2 us here.  The training-step operators allocate their outputs and workspaces here too
+// (a lookup of a short prompt: 11.5 us from Python, its kernel 2).
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -297,12 +299,305 @@ PyObject *py_sweep_qualify(PyObject *, PyObject *const *args, Py_ssize_t n) {
     }
 }
 
+// ---- training-step operators --------------------------------------------------------------------------------------
+
+constexpr int kMaxDevices = 64;
+uint32_t *g_status[kMaxDevices];       // the status word of each device, set from Python
+
+// set_status(device, address)
+PyObject *py_set_status(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    long long dev, p;
+    if (!want_args(n, 2) || !to_ll(args[0], &dev) || !to_ll(args[1], &p)) return nullptr;
+    if (dev < 0 || dev >= kMaxDevices) {
+        PyErr_SetString(PyExc_ValueError, "device out of range");
+        return nullptr;
+    }
+    g_status[dev] = (uint32_t *)p;
+    Py_RETURN_NONE;
+}
+
+// A call's tensors: checks that set a Python error and return false, and outputs made or taken from the caller's mapping.
+struct Call {
+    int device = -1;
+    const at::Tensor *cuda(PyObject *o, const char *what) {
+        if (!THPVariable_Check(o) || !THPVariable_Unpack(o).is_cuda()) {
+            PyErr_Format(PyExc_ValueError, "%s must be a CUDA tensor", what);
+            return nullptr;
+        }
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (device < 0) device = t.get_device();
+        if (t.get_device() != device) {
+            PyErr_Format(PyExc_ValueError, "%s is on cuda:%d, the other tensors on cuda:%d", what, (int)t.get_device(), device);
+            return nullptr;
+        }
+        return &t;
+    }
+    static int dtype(const at::Tensor &t, const char *what) {
+        if (t.scalar_type() == c10::kFloat) return GUARD_F32;
+        if (t.scalar_type() == c10::kBFloat16) return GUARD_BF16;
+        if (t.scalar_type() == c10::kHalf) return GUARD_F16;
+        PyErr_Format(PyExc_ValueError, "%s must be float32, bfloat16 or float16, got %s", what, c10::toString(t.scalar_type()));
+        return -1;
+    }
+    // Distance of the rows of a matrix whose rows are contiguous, or -1.
+    static int64_t rows(const at::Tensor &t, const char *what) {
+        if (t.dim() != 2) {
+            PyErr_Format(PyExc_ValueError, "%s must be a matrix", what);
+            return -1;
+        }
+        const int64_t n = t.size(0), d = t.size(1);
+        if ((d > 1 && t.stride(1) != 1) || (n > 1 && t.stride(0) < d)) {
+            PyErr_Format(PyExc_ValueError, "%s must have contiguous rows that do not overlap", what);
+            return -1;
+        }
+        return n > 1 ? t.stride(0) : d;
+    }
+    static int token_bits(const at::Tensor &t, const char *what) {
+        const int bits = t.scalar_type() == c10::kLong ? 64 : t.scalar_type() == c10::kInt ? 32 : 0;
+        if (!bits || !t.is_contiguous()) {
+            PyErr_Format(PyExc_ValueError, "%s must be contiguous, int32 or int64", what);
+            return 0;
+        }
+        return bits;
+    }
+    bool flat(PyObject *o, const char *what, c10::ScalarType type, int64_t numel, void **to) {
+        const at::Tensor *t = cuda(o, what);
+        if (!t) return false;
+        if (t->scalar_type() != type || !t->is_contiguous() || t->numel() != numel) {
+            PyErr_Format(PyExc_ValueError, "%s must be contiguous, of %s and of %lld elements", what, c10::toString(type), (long long)numel);
+            return false;
+        }
+        *to = t->data_ptr();
+        return true;
+    }
+    at::Tensor make(at::IntArrayRef size, c10::ScalarType type) const {
+        return at::empty(size, at::TensorOptions().dtype(type).device(c10::Device(c10::kCUDA, (c10::DeviceIndex)device)));
+    }
+    // An entry of the caller's mapping (NULL pointer: missing or None; allowed only where optional), or, without a mapping, a
+    // new tensor that is put into `made`.
+    bool output(PyObject *out, PyObject *made, const char *name, c10::ScalarType type, at::IntArrayRef size, bool optional, void **to) {
+        int64_t numel = 1;
+        for (int64_t d : size) numel *= d;
+        *to = nullptr;
+        if (out == Py_None) {
+            at::Tensor t = make(size, type);
+            *to = t.data_ptr();
+            Ref w{THPVariable_Wrap(std::move(t))};
+            return w.o && PyDict_SetItemString(made, name, w.o) == 0;
+        }
+        Ref v{PyObject_CallMethod(out, "get", "s", name)};
+        if (!v.o) return false;
+        if (v.o == Py_None) {
+            if (optional) return true;
+            PyErr_Format(PyExc_ValueError, "out['%s'] is missing", name);
+            return false;
+        }
+        return flat(v.o, name, type, numel, to);
+    }
+    bool workspace(PyObject *given, size_t need, at::Tensor &keep, void **p, size_t *bytes) {
+        if (given == Py_None) {
+            if (need) keep = make({(int64_t)need}, c10::kByte);
+            *p = need ? keep.data_ptr() : nullptr;
+            *bytes = need;
+            return true;
+        }
+        const at::Tensor *t = cuda(given, "workspace");
+        if (!t) return false;
+        if (t->scalar_type() != c10::kByte || !t->is_contiguous()) {
+            PyErr_SetString(PyExc_ValueError, "workspace must be contiguous, of torch.uint8");
+            return false;
+        }
+        *p = t->data_ptr();
+        *bytes = (size_t)t->numel();
+        return true;
+    }
+    bool status(PyObject *out, uint32_t **p) {
+        *p = device >= 0 && device < kMaxDevices ? g_status[device] : nullptr;
+        if (out == Py_None) return true;
+        Ref v{PyObject_CallMethod(out, "get", "s", "status")};
+        if (!v.o) return false;
+        void *q;
+        if (v.o == Py_None) return true;
+        if (!flat(v.o, "status", c10::kUInt32, 1, &q)) return false;
+        *p = (uint32_t *)q;
+        return true;
+    }
+};
+
+// The mapping of outputs, or the error code of the C call.
+PyObject *result(int rc, PyObject *out, Ref &made) {
+    if (rc != GUARD_OK) return PyLong_FromLong(rc);
+    if (out == Py_None) return made.give();
+    Py_INCREF(out);
+    return out;
+}
+
+// embed(tokens, table, scale, out) -> outputs or status
+PyObject *py_embed(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (!want_args(n, 4)) return nullptr;
+    const double scale = PyFloat_AsDouble(args[2]);
+    if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+    try {
+        Call c;
+        const at::Tensor *table = c.cuda(args[1], "table"), *tokens = table ? c.cuda(args[0], "tokens") : nullptr;
+        if (!tokens) return nullptr;
+        const int bits = Call::token_bits(*tokens, "tokens"), code = bits ? Call::dtype(*table, "table") : -1;
+        const int64_t stride = code >= 0 ? Call::rows(*table, "table") : -1;
+        if (stride < 0) return nullptr;
+        const int64_t width = table->size(1);
+        Here here(c.device);
+        Ref made{PyDict_New()};
+        c10::SmallVector<int64_t, 6> size(tokens->sizes().begin(), tokens->sizes().end());
+        size.push_back(width);
+        void *to;
+        uint32_t *status;
+        if (!made.o || !c.output(args[3], made.o, "out", table->scalar_type(), size, false, &to) || !c.status(args[3], &status)) return nullptr;
+        const int rc = guard_embed(tokens->data_ptr(), bits, tokens->numel(), table->data_ptr(), table->size(0), width, stride, code, (float)scale, to,
+                                   status, here.stream);
+        return result(rc, args[3], made);
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+// embed_grad(grad, tokens, rows, scale, padding_idx, accumulate, workspace, out) -> outputs or status
+PyObject *py_embed_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    long long rows, padding;
+    if (!want_args(n, 8) || !to_ll(args[2], &rows) || !to_ll(args[4], &padding)) return nullptr;
+    const double scale = PyFloat_AsDouble(args[3]);
+    if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+    const int accumulate = PyObject_IsTrue(args[5]);
+    if (accumulate < 0) return nullptr;
+    try {
+        Call c;
+        const at::Tensor *given = c.cuda(args[0], "grad"), *tokens = given ? c.cuda(args[1], "tokens") : nullptr;
+        if (!tokens) return nullptr;
+        at::Tensor grad = *given;
+        if (grad.dim() != 2 && grad.dim() > 0 && grad.is_contiguous() && grad.size(-1) > 0) grad = grad.view({-1, grad.size(-1)});
+        const int bits = Call::token_bits(*tokens, "tokens"), code = bits ? Call::dtype(grad, "grad") : -1;
+        const int64_t stride = code >= 0 ? Call::rows(grad, "grad") : -1;
+        if (stride < 0) return nullptr;
+        const int64_t count = grad.size(0), width = grad.size(1);
+        if (tokens->numel() != count) {
+            PyErr_Format(PyExc_ValueError, "%lld gradient rows for %lld tokens", (long long)count, (long long)tokens->numel());
+            return nullptr;
+        }
+        if (accumulate && args[7] == Py_None) {
+            PyErr_SetString(PyExc_ValueError, "accumulate needs out['dtable']");
+            return nullptr;
+        }
+        Here here(c.device);
+        Ref made{PyDict_New()};
+        void *to, *ws;
+        uint32_t *status;
+        size_t bytes;
+        at::Tensor keep;
+        const size_t need = guard_embed_grad_workspace_bytes(count, rows, width);
+        if (need == 0) return PyLong_FromLong(guard_embed_grad(nullptr, stride, code, nullptr, bits, count, rows, width, 1.0f, -1, 0, nullptr, nullptr, 0, nullptr, nullptr));
+        if (!made.o || !c.output(args[7], made.o, "dtable", grad.scalar_type(), {rows, width}, false, &to) || !c.workspace(args[6], need, keep, &ws, &bytes) ||
+            !c.status(args[7], &status))
+            return nullptr;
+        const int rc = guard_embed_grad(grad.data_ptr(), stride, code, tokens->data_ptr(), bits, count, rows, width, (float)scale, padding, accumulate, to, ws, bytes,
+                                        status, here.stream);
+        return result(rc, args[7], made);
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+// The product's inputs, as both directions take them.
+struct Product {
+    const at::Tensor *x = nullptr, *w = nullptr, *targets = nullptr;
+    int bits = 0, code = -1;
+    int64_t xs = -1, ws = -1, rows = 0, width = 0, vocab = 0;
+    bool read(Call &c, PyObject *const *args) {
+        if (!(x = c.cuda(args[0], "x")) || !(w = c.cuda(args[1], "w")) || !(targets = c.cuda(args[2], "targets")) || !(bits = Call::token_bits(*targets, "targets")) ||
+            (code = Call::dtype(*x, "x")) < 0)
+            return false;
+        if (w->scalar_type() != x->scalar_type() || code == GUARD_F32) {
+            PyErr_Format(PyExc_ValueError, "x and w must both be bfloat16 or both float16, got %s and %s", c10::toString(x->scalar_type()), c10::toString(w->scalar_type()));
+            return false;
+        }
+        if ((xs = Call::rows(*x, "x")) < 0 || (ws = Call::rows(*w, "w")) < 0) return false;
+        rows = x->size(0), width = x->size(1), vocab = w->size(0);
+        if (w->size(1) != width || targets->numel() != rows) {
+            PyErr_SetString(PyExc_ValueError, "need x [rows, width], w [vocab, width] and rows targets");
+            return false;
+        }
+        return true;
+    }
+};
+
+// linear_xent(x, w, targets, ignore_index, workspace, out) -> outputs or status
+PyObject *py_linear_xent(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    long long ignore;
+    if (!want_args(n, 6) || !to_ll(args[3], &ignore)) return nullptr;
+    try {
+        Call c;
+        Product p;
+        if (!p.read(c, args)) return nullptr;
+        Here here(c.device);
+        Ref made{PyDict_New()};
+        void *loss, *lse, *ws;
+        uint32_t *status;
+        size_t bytes;
+        at::Tensor keep;
+        if (!made.o || !c.output(args[5], made.o, "loss", c10::kFloat, {p.rows}, false, &loss) || !c.output(args[5], made.o, "lse", c10::kFloat, {p.rows}, false, &lse) ||
+            !c.workspace(args[4], guard_linear_xent_workspace_bytes(p.rows, p.width, p.vocab, 0), keep, &ws, &bytes) || !c.status(args[5], &status))
+            return nullptr;
+        const int rc = guard_linear_xent(p.x->data_ptr(), p.xs, p.w->data_ptr(), p.ws, p.rows, p.width, p.vocab, p.code, p.targets->data_ptr(), p.bits, ignore,
+                                         (float *)loss, (float *)lse, ws, bytes, status, here.stream);
+        return result(rc, args[5], made);
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+// linear_xent_grad(x, w, targets, lse, grad_loss, ignore_index, workspace, out) -> outputs or status
+PyObject *py_linear_xent_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    long long ignore;
+    if (!want_args(n, 8) || !to_ll(args[5], &ignore)) return nullptr;
+    try {
+        Call c;
+        Product p;
+        if (!p.read(c, args)) return nullptr;
+        Here here(c.device);
+        Ref made{PyDict_New()};
+        void *dx, *dw, *lse, *g, *ws;
+        uint32_t *status;
+        size_t bytes;
+        at::Tensor keep;
+        const at::Tensor *grad = c.cuda(args[4], "grad_loss");
+        if (!grad) return nullptr;
+        const bool one = grad->numel() == 1 && p.rows != 1;
+        if (!made.o || !c.flat(args[3], "lse", c10::kFloat, p.rows, &lse) || !c.flat(args[4], "grad_loss", c10::kFloat, one ? 1 : p.rows, &g) ||
+            !c.output(args[7], made.o, "dx", p.x->scalar_type(), {p.rows, p.width}, true, &dx) ||
+            !c.output(args[7], made.o, "dw", p.w->scalar_type(), {p.vocab, p.width}, true, &dw) ||
+            !c.workspace(args[6], guard_linear_xent_workspace_bytes(p.rows, p.width, p.vocab, 1), keep, &ws, &bytes) || !c.status(args[7], &status))
+            return nullptr;
+        const int rc = guard_linear_xent_grad(p.x->data_ptr(), p.xs, p.w->data_ptr(), p.ws, p.rows, p.width, p.vocab, p.code, p.targets->data_ptr(), p.bits, ignore,
+                                              (const float *)lse, (const float *)g, one ? 0 : 1, dx, dw, ws, bytes, status, here.stream);
+        return result(rc, args[7], made);
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
 PyMethodDef g_methods[] = {{"current_stream", (PyCFunction)(void (*)(void))py_current_stream, METH_FASTCALL, nullptr},
                            {"ingest", (PyCFunction)(void (*)(void))py_ingest, METH_FASTCALL, nullptr},
                            {"score", (PyCFunction)(void (*)(void))py_score, METH_FASTCALL, nullptr},
                            {"node_verdict", (PyCFunction)(void (*)(void))py_node_verdict, METH_FASTCALL, nullptr},
                            {"join", (PyCFunction)(void (*)(void))py_join, METH_FASTCALL, nullptr},
                            {"sweep_qualify", (PyCFunction)(void (*)(void))py_sweep_qualify, METH_FASTCALL, nullptr},
+                           {"set_status", (PyCFunction)(void (*)(void))py_set_status, METH_FASTCALL, nullptr},
+                           {"embed", (PyCFunction)(void (*)(void))py_embed, METH_FASTCALL, nullptr},
+                           {"embed_grad", (PyCFunction)(void (*)(void))py_embed_grad, METH_FASTCALL, nullptr},
+                           {"linear_xent", (PyCFunction)(void (*)(void))py_linear_xent, METH_FASTCALL, nullptr},
+                           {"linear_xent_grad", (PyCFunction)(void (*)(void))py_linear_xent_grad, METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_guard_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -47,7 +47,8 @@ enum Mode { kStats, kGrad, kDx, kDw };
 struct Header {         // at the start of the workspace, written by xent_rows_kernel
     int32_t count;      // rows that take part
     int32_t whole;      // they are all rows: x is read where it is
-    float inverse;      // what a gradient from G is multiplied by
+    float unit, scale;  // G holds g / unit * scale
+    float inverse;      // what a gradient from G is multiplied by: unit / scale
 };
 
 struct ProductArgs {
@@ -61,7 +62,7 @@ struct ProductArgs {
     const int32_t *target; // [rows] vocabulary index or -1, by (gathered) row
     const void *raw_target;   // without a header: int32 or int64 as the caller gave them
     int target_bits;
-    const float *lse, *grad;  // [rows], by gathered row: log sums and scaled row gradients
+    const float *lse, *grad;  // [rows], by gathered row: log sums and row gradients
     float2 *parts;         // [rows][n_parts] largest value and sum
     int n_parts;
     float *picked;         // [rows] logit of the target
@@ -293,7 +294,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         // ---- what becomes of an accumulator: a thread has a row, and half of its columns
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const uint32_t mine = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
-        const float inverse = a.head ? a.head->inverse : 1.0f;
+        const float inverse = a.head ? a.head->inverse : 1.0f, unit = a.head ? a.head->unit : 1.0f, scale = a.head ? a.head->scale : 1.0f;
         const uint32_t free0 = in_first(&s.free_[0]), free1 = in_first(&s.free_[1]);
         uint32_t nth = 0;
         for (int t = pair; t < total; t += pairs) {
@@ -310,7 +311,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     else target = a.target_bits == 64 ? reinterpret_cast<const long long *>(a.raw_target)[row] : reinterpret_cast<const int *>(a.raw_target)[row];
                     if (MODE == kGrad) {
                         lse2 = __fmul_rn(a.lse[row], kLog2e);
-                        g = a.grad[row];
+                        g = __fmul_rn(__fdiv_rn(a.grad[row], unit), scale);
                     }
                 }
             }
@@ -451,68 +452,79 @@ __device__ __forceinline__ int64_t target_at(const void *t, int bits, int64_t i)
     return bits == 64 ? reinterpret_cast<const long long *>(t)[i] : (int64_t) reinterpret_cast<const int *>(t)[i];
 }
 
-// One CTA walks over the rows in order.
+// One CTA walks over the rows in order, eight a thread at a time.
 __global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a) {
+    constexpr int kEach = 8;
     __shared__ int s_count[32];
     __shared__ float s_top[32];
     pdl_wait();
     const int lane = lane_id(), warp = warp_id();
-    float unit = 1.0f, scale = 1.0f;      // G holds g / unit * scale
-    if (a.grads) {
-        float top = 0.0f;
-        for (int i = threadIdx.x; i < a.rows; i += 1024) {
-            const int64_t t = target_at(a.targets, a.bits, i);
-            if (t != a.ignore && t >= 0 && t < a.vocab) top = fmaxf(top, fabsf(a.grad[i * a.grad_stride]));
-        }
-        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-        if (lane == 0) s_top[warp] = top;
-        __syncthreads();
-        for (int w = 0; w < 32; ++w) top = fmaxf(top, s_top[w]);
-        if (top >= 1e-30f && top < INFINITY) {     // (else the products below could leave float32's range)
-            unit = top;
-            if (a.half) scale = 32768.0f;
-        }
-    }
     int before = 0;
-    for (int64_t base = 0; base < a.rows; base += 1024) {
-        const int64_t i = base + threadIdx.x;
-        bool in = false;
-        int64_t t = -1;
-        if (i < a.rows) {
-            t = target_at(a.targets, a.bits, i);
-            const bool bad = t != a.ignore && (t < 0 || t >= a.vocab);
-            in = t != a.ignore && !bad;
-            if (bad && a.status) atomicOr(a.status, kStatIndex);
-            if (!in && a.loss) {
-                a.loss[i] = bad ? __uint_as_float(0x7FC00000u) : 0.0f;
-                a.lse_out[i] = 0.0f;
+    float top = 0.0f;
+    for (int64_t base = 0; base < a.rows; base += 1024 * kEach) {
+        const int64_t first = base + threadIdx.x * kEach;
+        int64_t t[kEach];
+        float g[kEach];
+        uint32_t in = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            t[j] = first + j < a.rows ? target_at(a.targets, a.bits, first + j) : a.ignore;
+            g[j] = a.grads && first + j < a.rows ? a.grad[(first + j) * a.grad_stride] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const bool bad = t[j] != a.ignore && (t[j] < 0 || t[j] >= a.vocab);
+            if (t[j] != a.ignore && !bad) {
+                in |= 1u << j;
+                top = fmaxf(top, fabsf(g[j]));
+            } else if (first + j < a.rows) {
+                if (bad && a.status) atomicOr(a.status, kStatIndex);
+                if (a.loss) {
+                    a.loss[first + j] = bad ? __uint_as_float(0x7FC00000u) : 0.0f;
+                    a.lse_out[first + j] = 0.0f;
+                }
             }
         }
-        const uint32_t votes = __ballot_sync(0xFFFFFFFFu, in);
-        if (lane == 0) s_count[warp] = __popc(votes);
+        const int mine = __popc(in);
+        int upto = mine;
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+            if (lane >= d) upto += y;
+        }
+        if (lane == 31) s_count[warp] = upto;
         __syncthreads();
-        int at = before, all = 0;
-        for (int w = 0; w < 32; ++w) {
-            if (w < warp) at += s_count[w];
-            all += s_count[w];
-        }
-        at += __popc(votes & ((1u << lane) - 1));
-        if (in) {
-            a.target[at] = (int32_t)t;
-            a.row_of[at] = (int32_t)i;
-            if (a.lse_to) {
-                a.lse_to[at] = a.lse[i];
-                a.grad_to[at] = __fmul_rn(__fdiv_rn(a.grad[i * a.grad_stride], unit), scale);
+        const int other = s_count[lane];
+        const int all = __reduce_add_sync(0xFFFFFFFFu, other);
+        int at = before + upto - mine + __reduce_add_sync(0xFFFFFFFFu, lane < warp ? other : 0);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            if (first + j >= a.rows) continue;
+            const bool takes = (in >> j) & 1;
+            if (takes) {
+                a.target[at] = (int32_t)t[j];
+                a.row_of[at] = (int32_t)(first + j);
+                if (a.grads) {
+                    a.lse_to[at] = a.lse[first + j];
+                    a.grad_to[at] = g[j];
+                }
             }
+            a.place[first + j] = takes ? at : -1;
+            at += takes;
         }
-        if (i < a.rows) a.place[i] = in ? at : -1;
         before += all;
         __syncthreads();
     }
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+    if (lane == 0) s_top[warp] = top;
+    __syncthreads();
     if (threadIdx.x == 0) {
+        for (int w = 0; w < 32; ++w) top = fmaxf(top, s_top[w]);
+        const bool plain = !(top >= 1e-30f && top < INFINITY);     // (the products could leave float32's range)
         a.head->count = before;
         a.head->whole = before == a.rows;
-        a.head->inverse = __fdiv_rn(unit, scale);
+        a.head->unit = plain ? 1.0f : top;
+        a.head->scale = a.half && !plain ? 32768.0f : 1.0f;
+        a.head->inverse = __fdiv_rn(a.head->unit, a.head->scale);
     }
 }
 

@@ -22,7 +22,6 @@ from .guard import GUARD_OK, GuardError
 STATUS_TIMEOUT, STATUS_INDEX = 2, 8
 BLOCK = 256                 # elements to a scale of AdamW's 8-bit states; tensors start on such blocks of the flat states
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-_TOKENS = {torch.int32: 32, torch.int64: 64}
 
 
 class _AdamwTensor(C.Structure):
@@ -83,16 +82,6 @@ def _dtype(t: torch.Tensor, what: str) -> int:
     return code
 
 
-def _rows(t: torch.Tensor, what: str) -> int:
-    """Distance of the rows of a matrix whose rows are contiguous."""
-    if t.dim() != 2:
-        raise ValueError("%s must be a matrix" % what)
-    n, d = t.shape
-    if d > 1 and t.stride(1) != 1 or n > 1 and t.stride(0) < d:
-        raise ValueError("%s must have contiguous rows that do not overlap" % what)
-    return t.stride(0) if n > 1 else d
-
-
 def _contiguous(t: torch.Tensor, what: str, dtype: torch.dtype, numel: int, device: torch.device) -> int:
     _cuda(t, what, device)
     if t.dtype != dtype or not t.is_contiguous() or t.numel() != numel:
@@ -100,44 +89,34 @@ def _contiguous(t: torch.Tensor, what: str, dtype: torch.dtype, numel: int, devi
     return t.data_ptr()
 
 
-def _tokens(t: torch.Tensor, device: torch.device) -> int:
-    _cuda(t, "tokens", device)
-    bits = _TOKENS.get(t.dtype)
-    if bits is None or not t.is_contiguous():
-        raise ValueError("tokens must be contiguous, int32 or int64")
-    return bits
-
-
-def _workspace(given: Optional[torch.Tensor], need: int, device: torch.device) -> torch.Tensor:
-    if need == 0:
-        raise GuardError(-1, "invalid sizes")
-    if given is None:
-        return torch.empty(need, dtype=torch.uint8, device=device)
-    _cuda(given, "workspace", device)
-    if given.dtype != torch.uint8 or not given.is_contiguous():
-        raise ValueError("workspace must be contiguous, of torch.uint8")
-    return given
-
-
 _status: Dict[int, torch.Tensor] = {}
+_nat = None
 
 
-def _status_ptr(out, device: torch.device) -> int:
-    given = out.get("status") if out is not None else None
-    if given is not None:
-        return _contiguous(given, "status", torch.uint32, 1, device)
-    word = _status.get(device.index)
-    if word is None:
+def _call(name, first, *args):
+    """A native call, its device's status word in place before: the mapping of outputs."""
+    global _nat
+    if not isinstance(first, torch.Tensor) or not first.is_cuda:
+        raise ValueError("expected CUDA tensors")
+    dev = first.get_device()
+    if dev not in _status:
         if torch.cuda.is_current_stream_capturing():
-            raise RuntimeError("make the first call on a device before capturing, or pass out['status']")
-        word = _status[device.index] = torch.zeros(1, dtype=torch.int32, device=device)
-        torch.cuda.current_stream(device).synchronize()      # other streams may use it from now on
-    return word.data_ptr()
+            raise RuntimeError("make the first call on a device before capturing")
+        lib()
+        word = torch.zeros(1, dtype=torch.int32, device=first.device)
+        torch.cuda.current_stream(dev).synchronize()      # any stream may use it from now on
+        _nat = guard._native()
+        _nat.set_status(dev, word.data_ptr())
+        _status[dev] = word
+    r = getattr(_nat, name)(first, *args)
+    if r.__class__ is int:
+        _check(r)
+    return r
 
 
 def sync_status(device=None) -> None:
     """Waits for the current stream of `device`, raises GuardError if a call before met an error in its data, and clears
-    the device's status word."""
+    the device's status word.  (Calls still running on other streams meanwhile may set it before or after.)"""
     index = torch.device(device if device is not None else "cuda").index
     index = torch.cuda.current_device() if index is None else index
     word = _status.get(index)
@@ -156,16 +135,7 @@ def embed(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.0,
           out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
     """out["out"][...] = scale * table[tokens[...]]: rows of table [rows, width], any shape of tokens.  A token outside the
     table gives a row of NaN."""
-    dev = _cuda(table, "table")
-    bits, code, stride = _tokens(tokens, dev), _dtype(table, "table"), _rows(table, "table")
-    rows, width = table.shape
-    with _here(dev):
-        if out is None:
-            out = {"out": torch.empty((*tokens.shape, width), dtype=table.dtype, device=dev)}
-        to = _contiguous(out["out"], "out", table.dtype, tokens.numel() * width, dev)
-        _check(lib().guard_embed(tokens.data_ptr(), bits, tokens.numel(), table.data_ptr(), rows, width, stride, code, scale, to,
-                                 _status_ptr(out, dev), guard._stream()))
-    return out
+    return _call("embed", tokens, table, scale, out)
 
 
 def embed_grad(grad: torch.Tensor, tokens: torch.Tensor, rows: int, *, scale: float = 1.0, padding_idx: int = -1,
@@ -174,36 +144,7 @@ def embed_grad(grad: torch.Tensor, tokens: torch.Tensor, rows: int, *, scale: fl
     """out["dtable"][v] = scale * sum of grad[i] over tokens[i] == v, [rows, width] of grad's type; with accumulate, added
     to what out["dtable"] holds (rows without tokens stay as they are).  grad: [tokens, width], or contiguous of
     [..., width].  Tokens equal to padding_idx add nothing."""
-    dev = _cuda(grad, "grad")
-    if grad.dim() != 2 and grad.dim() > 0 and grad.is_contiguous():
-        grad = grad.view(-1, grad.shape[-1])
-    bits, code, stride = _tokens(tokens, dev), _dtype(grad, "grad"), _rows(grad, "grad")
-    n, width = grad.shape
-    if tokens.numel() != n:
-        raise ValueError("%d gradient rows for %d tokens" % (n, tokens.numel()))
-    with _here(dev):
-        if out is None:
-            if accumulate:
-                raise ValueError("accumulate needs out['dtable']")
-            out = {"dtable": torch.empty((rows, width), dtype=grad.dtype, device=dev)}
-        to = _contiguous(out["dtable"], "dtable", grad.dtype, rows * width, dev)
-        ws = _workspace(workspace, lib().guard_embed_grad_workspace_bytes(n, rows, width), dev)
-        _check(lib().guard_embed_grad(grad.data_ptr(), stride, code, tokens.data_ptr(), bits, n, rows, width, scale, padding_idx,
-                                      1 if accumulate else 0, to, ws.data_ptr(), ws.numel(), _status_ptr(out, dev), guard._stream()))
-    return out
-
-
-def _product(x, w, targets):
-    dev = _cuda(x, "x")
-    _cuda(w, "w", dev)
-    bits = _tokens(targets, dev)
-    code = _dtype(x, "x")
-    if w.dtype != x.dtype or code == 0:
-        raise ValueError("x and w must both be bfloat16 or both float16, got %s and %s" % (x.dtype, w.dtype))
-    xs, wst = _rows(x, "x"), _rows(w, "w")
-    if x.shape[1] != w.shape[1] or targets.numel() != x.shape[0]:
-        raise ValueError("need x [rows, width], w [vocab, width] and rows targets")
-    return dev, bits, code, xs, wst
+    return _call("embed_grad", grad, tokens, rows, scale, padding_idx, accumulate, workspace, out)
 
 
 def linear_xent(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, *, ignore_index: int = -100,
@@ -211,19 +152,7 @@ def linear_xent(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, *, igno
     """Softmax cross entropy of the logits x @ w.T against targets, row by row, without keeping the logits: float32
     out["loss"] and out["lse"] (the logits' log sum of exponentials, which the gradient takes).  x [rows, width] and
     w [vocab, width]: bfloat16 or float16, width a multiple of 8.  Rows whose target is ignore_index have 0 in both."""
-    dev, bits, code, xs, wst = _product(x, w, targets)
-    rows, width = x.shape
-    with _here(dev):
-        if out is None:
-            out = {"loss": torch.empty(rows, dtype=torch.float32, device=dev), "lse": torch.empty(rows, dtype=torch.float32, device=dev)}
-        loss = _contiguous(out["loss"], "loss", torch.float32, rows, dev)
-        lse = _contiguous(out["lse"], "lse", torch.float32, rows, dev)
-        if rows == 0:
-            return out
-        ws = _workspace(workspace, lib().guard_linear_xent_workspace_bytes(rows, width, w.shape[0], 0), dev)
-        _check(lib().guard_linear_xent(x.data_ptr(), xs, w.data_ptr(), wst, rows, width, w.shape[0], code, targets.data_ptr(), bits, ignore_index,
-                                       loss, lse, ws.data_ptr(), ws.numel(), _status_ptr(out, dev), guard._stream()))
-    return out
+    return _call("linear_xent", x, w, targets, ignore_index, workspace, out)
 
 
 def linear_xent_grad(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, grad_loss: torch.Tensor, *,
@@ -231,23 +160,7 @@ def linear_xent_grad(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, ls
                      out: Optional[Dict[str, Optional[torch.Tensor]]] = None) -> Dict[str, Optional[torch.Tensor]]:
     """Gradients of (grad_loss * loss).sum(): out["dx"] and out["dw"], of the inputs' type (a missing or None entry of `out`
     is skipped).  lse: as linear_xent gave it; grad_loss: float32, one value per row, or one for all."""
-    dev, bits, code, xs, wst = _product(x, w, targets)
-    rows, width = x.shape
-    vocab = w.shape[0]
-    with _here(dev):
-        if out is None:
-            out = {"dx": torch.empty((rows, width), dtype=x.dtype, device=dev), "dw": torch.empty((vocab, width), dtype=w.dtype, device=dev)}
-        dx, dw = out.get("dx"), out.get("dw")
-        pdx = None if dx is None else _contiguous(dx, "dx", x.dtype, rows * width, dev)
-        pdw = None if dw is None else _contiguous(dw, "dw", w.dtype, vocab * width, dev)
-        plse = _contiguous(lse, "lse", torch.float32, rows, dev)
-        one = grad_loss.numel() == 1 and rows != 1
-        pg = _contiguous(grad_loss, "grad_loss", torch.float32, 1 if one else rows, dev)
-        ws = _workspace(workspace, lib().guard_linear_xent_workspace_bytes(rows, width, vocab, 1), dev) if rows else None
-        _check(lib().guard_linear_xent_grad(x.data_ptr(), xs, w.data_ptr(), wst, rows, width, vocab, code, targets.data_ptr(), bits, ignore_index,
-                                            plse, pg, 0 if one else 1, pdx, pdw, ws.data_ptr() if rows else None, ws.numel() if rows else 0,
-                                            _status_ptr(out, dev), guard._stream()))
-    return out
+    return _call("linear_xent_grad", x, w, targets, lse, grad_loss, ignore_index, workspace, out)
 
 
 class AdamW:

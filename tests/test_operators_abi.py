@@ -48,6 +48,31 @@ def test_embed_grad_refusals(L):
         assert call(**bad) == -2, bad
 
 
+def test_cross_entropy_refusals(L):
+    need = {g: L.guard_linear_xent_workspace_bytes(300, 64, 1000, g) for g in (0, 1)}
+    assert need[0] > 0 and need[1] > need[0] and need[0] % 256 == 0 and need[1] % 256 == 0
+    for bad in ((0, 64, 1000), (300, 0, 1000), (300, 60, 1000), (300, 64, 0), (1 << 31, 64, 1000), (300, 64, 1 << 31), (1 << 30, 64, 1 << 30), (300, 1 << 25, 1000)):
+        assert L.guard_linear_xent_workspace_bytes(*bad, 0) == 0, bad
+    big = 1 << 40
+    def forward(x=P, xs=64, w=Q, wst=64, n=300, d=64, v=1000, dtype=1, t=WS, bits=64, loss=WS + big, lse=WS + big + 4096, ws=WS + 2 * big, nws=need[0]):
+        return L.guard_linear_xent(x, xs, w, wst, n, d, v, dtype, t, bits, -100, loss, lse, ws, nws, None, None)
+    def backward(x=P, xs=64, w=Q, wst=64, n=300, d=64, v=1000, dtype=1, t=WS, bits=64, lse=WS + big, g=WS + big + 4096, gs=1, dx=WS + 2 * big, dw=WS + 3 * big,
+                 ws=WS + 4 * big, nws=need[1]):
+        return L.guard_linear_xent_grad(x, xs, w, wst, n, d, v, dtype, t, bits, -100, lse, g, gs, dx, dw, ws, nws, None, None)
+    assert forward(n=0) == 0 and backward(n=0, dw=None) == 0
+    both = (dict(dtype=0), dict(dtype=3), dict(bits=16), dict(xs=56), dict(xs=68), dict(wst=60), dict(wst=0), dict(d=60), dict(n=-1), dict(v=0), dict(x=None), dict(w=None),
+            dict(t=None), dict(x=P + 2), dict(w=Q + 8), dict(t=WS + 4))
+    for bad in both + (dict(loss=None), dict(lse=None), dict(lse=WS + big + 2), dict(loss=P), dict(lse=WS + big + 100), dict(loss=WS + 8), dict(loss=WS + 2 * big)):
+        assert forward(**bad) == -1, bad
+        assert text(L)
+    for bad in both + (dict(lse=None), dict(g=None), dict(gs=2), dict(dx=None, dw=None), dict(dx=WS + 2 * big + 8), dict(dw=Q), dict(dx=P + 16), dict(dw=WS + 2 * big),
+                       dict(dx=WS + 4 * big), dict(dx=WS + big)):
+        assert backward(**bad) == -1, bad
+    for bad in (dict(ws=None), dict(ws=WS + 2 * big + 64), dict(nws=need[0] - 1)):
+        assert forward(**bad) == -2, bad
+    assert backward(nws=need[1] - 1) == -2
+
+
 def test_adamw_refusals(L):
     from paper_2605_17879_b200 import operators as ops
     h = C.c_void_p()
@@ -88,8 +113,8 @@ def test_binding_refusals(L):
         ops.AdamW([], [])
     with pytest.raises(ValueError):
         ops.AdamW([x], [x], state_bits=16)
-    for bad in (torch.zeros(8, 8)[:, ::2], torch.zeros(8).expand(4, 8), torch.zeros(8)):
-        with pytest.raises(ValueError):
-            ops._rows(bad, "table")
-    assert ops._rows(torch.zeros(8, 8)[:, :5], "table") == 8 and ops._rows(torch.zeros(1, 5).expand(1, 5), "table") == 5
+    with pytest.raises(ValueError):
+        ops.linear_xent(x, x, ids)
+    with pytest.raises(ValueError):
+        ops.linear_xent_grad(x, x, ids, x, x)
     assert ops.AdamW.state_blocks([torch.zeros(0), torch.zeros(257)]) == 2
