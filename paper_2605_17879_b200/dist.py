@@ -1,9 +1,9 @@
-"""Multi-process plumbing for the benchmark.
+"""Multi-process plumbing for the benchmark and the node sweep.
 
 The scoring path does not shard across GPUs (a cross-rank median needs every rank of a
 step on one device), so N GPUs run N independent replicas of the workload: no data-path
 collective exists.  The only communication is the benchmark's own barrier and the
-max-over-ranks reduction of the measured time.
+max-over-ranks reduction of the measured time, and the sweep's collection of every GPU's results.
 """
 from __future__ import annotations
 
@@ -57,6 +57,15 @@ def aggregate_throughput(units_this_rank: float, seconds_this_rank: float, devic
     total = sum_over_ranks(units_this_rank, device)
     tmax = max_over_ranks(seconds_this_rank, device)
     return total / tmax, tmax
+
+
+def gather(mine: torch.Tensor) -> torch.Tensor:
+    """Every rank's tensor (all of one shape), rank by rank along a new first dimension, on every rank."""
+    if not dist.is_initialized():
+        return mine.unsqueeze(0)
+    parts = [torch.empty_like(mine) for _ in range(dist.get_world_size())]
+    dist.all_gather(parts, mine.contiguous())
+    return torch.stack(parts)
 
 
 def finish() -> None:

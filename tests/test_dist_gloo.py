@@ -44,3 +44,38 @@ def test_single_process_is_identity():
     from paper_2605_17879_b200 import dist as gd
     assert gd.aggregate_throughput(10.0, 2.0) == (5.0, 2.0)
     assert gd.env_world()[2] >= 1
+
+
+def _gather_worker(rank, world, port, q):
+    os.environ.update(RANK=str(rank), LOCAL_RANK=str(rank), WORLD_SIZE=str(world), MASTER_ADDR="127.0.0.1",
+                      MASTER_PORT=str(port))
+    import torch
+    from paper_2605_17879_b200 import dist as gd
+    gd.init("gloo")
+    got = gd.gather(torch.full((3, 4), float(rank))[:, :2])      # (not contiguous)
+    q.put((rank, got.tolist()))
+    gd.barrier()
+    gd.finish()
+
+
+def test_gather_collects_every_ranks_rows():
+    with socket.socket() as s:
+        s.bind(("127.0.0.1", 0))
+        port = s.getsockname()[1]
+    ctx = mp.get_context("spawn")
+    q = ctx.Queue()
+    procs = [ctx.Process(target=_gather_worker, args=(r, 2, port, q)) for r in range(2)]
+    for p in procs:
+        p.start()
+    res = [q.get(timeout=120) for _ in procs]
+    for p in procs:
+        p.join(timeout=60)
+        assert p.exitcode == 0
+    for _, rows in res:
+        assert rows == [[[float(r)] * 2] * 3 for r in range(2)]
+
+
+def test_gather_of_a_single_process():
+    import torch
+    from paper_2605_17879_b200 import dist as gd
+    assert gd.gather(torch.ones(3, 4)).shape == (1, 3, 4)

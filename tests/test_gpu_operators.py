@@ -198,7 +198,7 @@ SHAPES = [[(1,)], [(256,)], [(255,), (0,), (257,)], [(300, 7), (1,), (1023,), (8
 
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("gtype,ctype", [(torch.bfloat16, torch.bfloat16), (torch.float16, None), (torch.float32, torch.float16), (torch.bfloat16, torch.float32)])
-@pytest.mark.parametrize("shapes", SHAPES, ids=str)
+@pytest.mark.parametrize("shapes", SHAPES, ids=lambda s: "%dx%s" % (len(s), s[0]))
 @pytest.mark.parametrize("shift", [0, 1])
 def test_adamw_step(ops, bits, gtype, ctype, shapes, shift):
     g = gen(len(shapes) + shift)
