@@ -23,8 +23,10 @@ __device__ __forceinline__ uint32_t in_first(const void *p) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(p)));
     return r;
 }
+// An arrival that orders no memory: for TMEM reads, which tcgen05.wait::ld and the fence before it have completed.  (The
+// releasing form waits for the thread's global stores to reach the whole GPU.)
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_address) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_address) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_address) : "memory");
 }
 // 2-D TMA load of a box at (x, y) into this CTA's memory, counted on a barrier of the pair (x, the innermost coordinate: a
 // multiple of 16 bytes of elements).
@@ -34,6 +36,14 @@ __device__ __forceinline__ void tma_load(void *dst, const CUtensorMap *map, int 
                  "l"(map), "r"(x), "r"(y), "r"(bar)
                  : "memory");
 }
+// 2-D TMA store of a box in shared memory to (x, y); what lies outside the matrix is not written.
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, const void *src, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(smem_u32(src)) : "memory");
+}
+__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }   // its memory may be written again
+__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_to_tma() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
 __device__ __forceinline__ void tmem_alloc(uint32_t *where, uint32_t columns) {   // one warp

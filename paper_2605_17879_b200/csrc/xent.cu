@@ -39,7 +39,8 @@ constexpr int kStage = 2 * kOperand;
 constexpr int kPass = 1024 / kK;              // stages that one accumulator takes in the forward pass
 constexpr int kEpilogueWarps = 8;
 constexpr int kProductThreads = 32 * (4 + kEpilogueWarps);
-constexpr int kProductSmem = kStages * kStage + 1024;
+constexpr int kBox = 32 * 128;                // bytes of what a warp stores at a time: 32 rows of 64 values
+constexpr int kProductSmem = kStages * kStage + kEpilogueWarps * kBox + 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 
 enum Mode { kStats, kGrad, kDx, kDw };
@@ -66,11 +67,10 @@ struct ProductArgs {
     float2 *parts;         // [rows][n_parts] largest value and sum
     int n_parts;
     float *picked;         // [rows] logit of the target
-    void *out;             // G, dx or dw
+    void *out;             // kDx: dx, where gathered rows are scattered
     int64_t out_stride;
     const int32_t *row_of; // gathered row -> row (dx)
-    float *partial;        // [splits][rows padded][width] (kDx)
-    int64_t partial_stride;
+    float4 *partial;       // kDx: partial sums by tile and split, as threads hold them (see partial_at)
     int add;               // add to partial
     int64_t width;
     uint32_t *status;
@@ -129,43 +129,56 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) 
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// 32 values of a row to 16-bit memory, those before `left`.
+// 32 values of a thread's row to 16-bit memory, those before `left` (a multiple of eight).
 template <typename T>
-__device__ __forceinline__ void store_row32(T *p, int left, bool wide, const float (&x)[32]) {
-    if (wide && left >= 32) {
+__device__ __forceinline__ void store_row32(T *p, int left, const float (&x)[32]) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            uint4 w;
-            w.x = pack2<T>(x[8 * q], x[8 * q + 1]);
-            w.y = pack2<T>(x[8 * q + 2], x[8 * q + 3]);
-            w.z = pack2<T>(x[8 * q + 4], x[8 * q + 5]);
-            w.w = pack2<T>(x[8 * q + 6], x[8 * q + 7]);
-            reinterpret_cast<uint4 *>(p)[q] = w;
-        }
-        return;
-    }
+    for (int q = 0; q < 4; ++q)
+        if (8 * q < left)
+            reinterpret_cast<uint4 *>(p)[q] = make_uint4(pack2<T>(x[8 * q], x[8 * q + 1]), pack2<T>(x[8 * q + 2], x[8 * q + 3]),
+                                                         pack2<T>(x[8 * q + 4], x[8 * q + 5]), pack2<T>(x[8 * q + 6], x[8 * q + 7]));
+}
+// 32 values of a thread's row to half `h` of the warp's box in shared memory (32 rows of 128 bytes, swizzled as TMA wants).
+template <typename T>
+__device__ __forceinline__ void box_row32(uint8_t *box, int h, const float (&x)[32]) {
+    const int row = lane_id();
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-        if (j < left) p[j] = Conv<T>::down(x[j]);
+    for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<uint4 *>(box + row * 128 + (((h * 4 + q) ^ (row & 7)) << 4)) =
+            make_uint4(pack2<T>(x[8 * q], x[8 * q + 1]), pack2<T>(x[8 * q + 2], x[8 * q + 3]), pack2<T>(x[8 * q + 4], x[8 * q + 5]),
+                       pack2<T>(x[8 * q + 6], x[8 * q + 7]));
+}
+
+// Partial sums of dx lie as the threads hold them: per tile and split 16 warps (rank, half, quarter), per warp 32 groups of
+// four columns, per group the 32 rows: every access of a warp is 512 bytes in a row.
+constexpr int64_t kPartialTile = (int64_t)kM * kN / 4;    // float4 of a tile
+__device__ __forceinline__ int64_t partial_at(int64_t unit, int rank, int half, int quarter, int group, int lane) {
+    return unit * kPartialTile + ((((rank * 2 + half) * 4 + quarter) * 32 + group) << 5) + lane;
 }
 
 // What a thread of the forward pass knows of its row: largest value so far, and the sum of exponentials relative to it.
 struct RowSum {
     float top, sum;
-    __device__ __forceinline__ void add(const float (&z)[32]) {
+    template <int N>
+    __device__ __forceinline__ void add(const float (&z)[N]) {
         float most = top;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) most = fmaxf(most, z[j]);
+        for (int j = 0; j < N; ++j) most = fmaxf(most, z[j]);
         const float base = finite_or_zero(most);
         const float shift = -__fmul_rn(base, kLog2e);
         if (sum != 0.0f) sum = __fmul_rn(sum, exp2_fast(__fmul_rn(__fsub_rn(finite_or_zero(top), base), kLog2e)));
         float part[4] = {};
 #pragma unroll
-        for (int j = 0; j < 32; ++j) part[j & 3] = __fadd_rn(part[j & 3], exp2_fast(__fmaf_rn(z[j], kLog2e, shift)));
+        for (int j = 0; j < N; ++j) part[j & 3] = __fadd_rn(part[j & 3], exp2_fast(__fmaf_rn(z[j], kLog2e, shift)));
         sum = __fadd_rn(sum, __fadd_rn(__fadd_rn(part[0], part[1]), __fadd_rn(part[2], part[3])));
         top = most;
     }
 };
+// y where j == at, else z; kept in registers (an indexed array would go to memory, tile by tile).
+__device__ __forceinline__ float pick(int j, int at, float y, float z) {
+    asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\tselp.f32 %0, %3, %0, p;\n\t}" : "+f"(z) : "r"(j), "r"(at), "f"(y));
+    return z;
+}
 
 // LONG: the depth takes more than one pass.  The tensor cores cut off what an accumulator's last bit cannot hold, product
 // step by product step, which shrinks a logit by some 2^-24 a step; the forward pass, whose results are float32, starts a new
@@ -174,7 +187,7 @@ struct RowSum {
 template <int MODE, bool LONG, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1) __cluster_dims__(2, 1, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a2, const __grid_constant__ CUtensorMap map_b,
-               const __grid_constant__ CUtensorMap map_b2, const ProductArgs a) {
+               const __grid_constant__ CUtensorMap map_b2, const __grid_constant__ CUtensorMap map_out, const ProductArgs a) {
     extern __shared__ uint8_t raw[];
     __shared__ ProductShared s;
     uint8_t *tiles = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
@@ -294,6 +307,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         // ---- what becomes of an accumulator: a thread has a row, and half of its columns
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const uint32_t mine = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
+        uint8_t *box = tiles + kStages * kStage + (warp - 4) * kBox;
         const float inverse = a.head ? a.head->inverse : 1.0f, unit = a.head ? a.head->unit : 1.0f, scale = a.head ? a.head->scale : 1.0f;
         const uint32_t free0 = in_first(&s.free_[0]), free1 = in_first(&s.free_[1]);
         uint32_t nth = 0;
@@ -341,85 +355,118 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             if (!__all_sync(0xFFFFFFFFu, wait_for(s, &s.done[acc], (nth >> 1) & 1))) break;
             ++nth;
             tc_fence_after();
-            RowSum sums{-INFINITY, 0.0f};
-            constexpr int kUnroll = LONG ? 4 : 1;
+            const uint32_t from = mine + acc * kN, freed = acc ? free1 : free0;
+            const int64_t col0 = (int64_t)tl.n * kN + half * 128;
+            if constexpr (MODE == kStats) {
+                RowSum sums{-INFINITY, 0.0f};
+                constexpr int N = LONG ? 16 : 32;
+                constexpr int kUnroll = LONG ? 128 / N : 1;
+                const int64_t left = a.vocab - col0;                     // columns that are there
+                const int at = (int)max((int64_t)-1, min((int64_t)128, target - col0));
 #pragma unroll kUnroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t r[32];
-                float x[32];
-                tmem_load32(mine + acc * kN + c * 32, r);
-                tmem_load_wait();
-                if (c == 3) {         // the accumulator is free once every warp has read its part
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_at(acc ? free1 : free0);
+                for (int c = 0; c < 128 / N; ++c) {
+                    uint32_t r[N];
+                    float z[N];
+                    if constexpr (LONG) tmem_load16(from + c * N, r);
+                    else tmem_load32(from + c * N, r);
+                    tmem_load_wait();
+                    if (c == 128 / N - 1) {         // the accumulator is free once every warp has read its part
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_at(freed);
+                    }
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        z[j] = __uint_as_float(r[j]);
+                        if constexpr (LONG) z[j] = __fadd_rn(held[c * N + j], z[j]);
+                    }
+                    if (left < (c + 1) * N) {
+#pragma unroll
+                        for (int j = 0; j < N; ++j)
+                            if (c * N + j >= left) z[j] = -INFINITY;
+                    }
+                    const bool here = at >= c * N && at < (c + 1) * N;
+                    if (__any_sync(0xFFFFFFFFu, here)) {
+                        float y = 0.0f;
+#pragma unroll
+                        for (int j = 0; j < N; ++j) y = pick(c * N + j, at, z[j], y);
+                        if (here) a.picked[row] = y;
+                    }
+                    sums.add(z);
                 }
-                const int64_t col = (int64_t)tl.n * kN + half * 128 + c * 32;
-                if (MODE == kStats || MODE == kGrad) {
-                    const int64_t first = a.v0 + col;
-                    const int64_t at = target - first;
-                    const bool here = at >= 0 && at < 32;
-                    const int left = (int)min((int64_t)32, max((int64_t)0, a.vocab - first));
-                    if (MODE == kStats) {
+                if (row < rows) a.parts[(int64_t)row * a.n_parts + tl.n * 2 + half] = make_float2(sums.top, sums.sum);
+            } else {
+                const bool partly = MODE == kDx && a.partial;
+                // (dx of gathered rows goes to the rows they come from; everything else is stored box by box)
+                const bool boxes = !partly && (MODE != kDx || whole);
+                const int64_t left = MODE == kGrad ? a.vocab - a.v0 - col0 : a.width - col0;     // columns that are there
+                const int at = (int)max((int64_t)-1, min((int64_t)128, target - a.v0 - col0));
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t r[32];
+                    float x[32];
+                    tmem_load32(from + c * 32, r);
+                    tmem_load_wait();
+                    if (c == 3) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_at(freed);
+                    }
+                    if constexpr (MODE == kGrad) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            x[j] = __uint_as_float(r[j]);
-                            if constexpr (LONG) x[j] = __fadd_rn(held[c * 32 + j], x[j]);
-                        }
-                        if (left < 32) {
+                        for (int j = 0; j < 32; ++j) x[j] = __fmul_rn(exp2_fast(__fmaf_rn(__uint_as_float(r[j]), kLog2e, -lse2)), g);
+                        const bool here = at >= c * 32 && at < (c + 1) * 32;
+                        if (__any_sync(0xFFFFFFFFu, here)) {             // the target: less one
 #pragma unroll
                             for (int j = 0; j < 32; ++j)
-                                if (j >= left) x[j] = -INFINITY;
-                        }
-                        if (__any_sync(0xFFFFFFFFu, here)) {
-                            float z = 0.0f;
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (j == (int)at) z = x[j];
-                            if (here) a.picked[row] = z;
-                        }
-                        sums.add(x);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            float p = exp2_fast(__fmaf_rn(__uint_as_float(r[j]), kLog2e, -lse2));
-                            if (j == (int)at && here) p = __fsub_rn(p, 1.0f);
-                            x[j] = j < left && row < rows ? __fmul_rn(p, g) : 0.0f;
+                                x[j] = pick(c * 32 + j, at, __fmul_rn(__fsub_rn(exp2_fast(__fmaf_rn(__uint_as_float(r[j]), kLog2e, -lse2)), 1.0f), g), x[j]);
                         }
                         // (G has whole tiles: its padding is written as zeros)
-                        store_row32(reinterpret_cast<T *>(a.out) + (int64_t)row * a.out_stride + col, 32, true, x);
-                    }
-                } else {
-                    const int left = (int)min((int64_t)32, max((int64_t)0, a.width - col));
-                    if (MODE == kDx && a.partial) {
-                        float *p = a.partial + tl.split * a.partial_stride + (int64_t)row * a.width + col;
-                        if (row < rows) {
+                        if (left < (c + 1) * 32 || row >= rows) {
 #pragma unroll
-                            for (int q = 0; q < 8; ++q)
-                                if (4 * q < left) {        // (the width is a multiple of eight)
-                                    float4 y = make_float4(__uint_as_float(r[4 * q]), __uint_as_float(r[4 * q + 1]), __uint_as_float(r[4 * q + 2]),
-                                                           __uint_as_float(r[4 * q + 3]));
-                                    if (empty) y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                                    if (a.add) {
-                                        const float4 z = reinterpret_cast<const float4 *>(p)[q];
-                                        y = make_float4(__fadd_rn(z.x, y.x), __fadd_rn(z.y, y.y), __fadd_rn(z.z, y.z), __fadd_rn(z.w, y.w));
-                                    }
-                                    reinterpret_cast<float4 *>(p)[q] = y;
-                                }
+                            for (int j = 0; j < 32; ++j)
+                                if (c * 32 + j >= left || row >= rows) x[j] = 0.0f;
                         }
+                    } else if (partly) {
+                        const int64_t unit = ((int64_t)tl.m * a.n_tiles + tl.n) * a.splits + tl.split;
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            float4 *p = a.partial + partial_at(unit, rank, half, quarter, c * 8 + q, lane);
+                            float4 y = make_float4(__uint_as_float(r[4 * q]), __uint_as_float(r[4 * q + 1]), __uint_as_float(r[4 * q + 2]), __uint_as_float(r[4 * q + 3]));
+                            if (empty) y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                            if (a.add) {
+                                const float4 z = *p;
+                                y = make_float4(__fadd_rn(z.x, y.x), __fadd_rn(z.y, y.y), __fadd_rn(z.z, y.z), __fadd_rn(z.w, y.w));
+                            }
+                            *p = y;
+                        }
+                        continue;
                     } else {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) x[j] = empty ? 0.0f : __fmul_rn(__uint_as_float(r[j]), inverse);
-                        const int64_t most = MODE == kDx ? rows : a.vocab - a.v0;     // rows of the result
-                        if (row < most) {
-                            const int64_t to = MODE == kDx ? (a.row_of && !whole ? a.row_of[row] : row) : a.v0 + row;
-                            store_row32(reinterpret_cast<T *>(a.out) + to * a.out_stride + col, left, true, x);
+                    }
+                    if (boxes) {
+                        if ((c & 1) == 0) {          // the box's memory, once the last store has read it
+                            if (lane == 0) tma_store_wait_read();
+                            __syncwarp();
                         }
+                        box_row32<T>(box, c & 1, x);
+                        if (c & 1) {
+                            fence_to_tma();
+                            __syncwarp();
+                            // (row: of lane 0, the box's first; a box that starts outside the result is not stored)
+                            if (lane == 0 && (MODE == kGrad || ((c - 1) * 32 < left && row < (MODE == kDx ? rows : a.vocab - a.v0)))) {
+                                tma_store(&map_out, box, (int)(col0 + (c - 1) * 32), (int)(MODE == kDw ? a.v0 + row : row));
+                                tma_store_commit();
+                            }
+                        }
+                    } else if (row < rows) {
+                        store_row32(reinterpret_cast<T *>(a.out) + (int64_t)a.row_of[row] * a.out_stride + col0 + c * 32, (int)min((int64_t)32, left - c * 32), x);
                     }
                 }
             }
-            if (MODE == kStats && row < rows) a.parts[(int64_t)row * a.n_parts + tl.n * 2 + half] = make_float2(sums.top, sums.sum);
         }
+        if (MODE != kStats && lane == 0) tma_store_wait();
     }
     tc_fence_before();
     __syncwarp();
@@ -625,36 +672,39 @@ __global__ void __launch_bounds__(256) xent_combine_kernel(const CombineArgs a) 
 struct JoinArgs {
     const Header *head;
     const int32_t *row_of;
-    int64_t rows, width;
-    const float *partial;
-    int64_t stride;
-    int splits;
+    int64_t width;
+    const float4 *partial;
+    int n_tiles, splits;
     void *dx;
 };
 
-// dx from its partial sums, in order.
+// dx from its partial sums, in order: a warp takes eight columns of 32 rows, in the products' layout.
 template <typename T>
 __global__ void __launch_bounds__(256) xent_join_kernel(const JoinArgs a) {
     pdl_wait();
-    const int64_t groups = a.width / 8, work = a.head->count * groups;
+    const int rows = a.head->count;
+    const int64_t m_tiles = (rows + kM - 1) / kM, work = m_tiles * a.n_tiles * 256;       // (16 warps of a tile, 16 pairs of groups)
     const float inverse = a.head->inverse;
     const bool whole = a.head->whole != 0;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < work; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / groups, col = (i - r * groups) * 8;
+    for (int64_t i = (int64_t)blockIdx.x * 8 + warp_id(); i < work; i += (int64_t)gridDim.x * 8) {
+        const int64_t tile = i >> 8;
+        const int part = (int)(i >> 4) & 15, pair = (int)i & 15;
+        const int rank = part >> 3, half = (part >> 2) & 1, quarter = part & 3;
+        const int64_t row = tile / a.n_tiles * kM + rank * kHalf + quarter * 32 + lane_id();
+        const int64_t col = tile % a.n_tiles * kN + half * 128 + pair * 8;
+        if (col >= a.width) continue;
         float x[8] = {};
         for (int k = 0; k < a.splits; ++k) {
-            const float4 *p = reinterpret_cast<const float4 *>(a.partial + k * a.stride + r * a.width + col);
-            const float4 u = p[0], v = p[1];
+            const float4 *p = a.partial + partial_at(tile * a.splits + k, rank, half, quarter, pair * 2, lane_id());
+            const float4 u = p[0], v = p[32];
             const float y[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = __fadd_rn(x[j], y[j]);
         }
-        uint4 w;
-        w.x = pack2<T>(__fmul_rn(x[0], inverse), __fmul_rn(x[1], inverse));
-        w.y = pack2<T>(__fmul_rn(x[2], inverse), __fmul_rn(x[3], inverse));
-        w.z = pack2<T>(__fmul_rn(x[4], inverse), __fmul_rn(x[5], inverse));
-        w.w = pack2<T>(__fmul_rn(x[6], inverse), __fmul_rn(x[7], inverse));
-        *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(a.dx) + (whole ? r : a.row_of[r]) * a.width + col) = w;
+        if (row >= rows) continue;
+        *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(a.dx) + (whole ? row : a.row_of[row]) * a.width + col) =
+            make_uint4(pack2<T>(__fmul_rn(x[0], inverse), __fmul_rn(x[1], inverse)), pack2<T>(__fmul_rn(x[2], inverse), __fmul_rn(x[3], inverse)),
+                       pack2<T>(__fmul_rn(x[4], inverse), __fmul_rn(x[5], inverse)), pack2<T>(__fmul_rn(x[6], inverse), __fmul_rn(x[7], inverse)));
     }
 }
 
@@ -691,7 +741,7 @@ constexpr int kDirectRows = kHalf;     // up to here the forward pass takes the 
 
 struct XentLayout {
     size_t head, target, row_of, place, lse, grad, picked, parts, x, g, partial, total;
-    int64_t padded, piece, partial_stride;
+    int64_t padded, piece;
     int n_parts, splits;
 };
 
@@ -728,26 +778,25 @@ XentLayout layout(int64_t rows, int64_t width, int64_t vocab, bool grads) {
         if (splits > depth / 4) splits = depth / 4;
         if (splits < 1) splits = 1;
         L.splits = (int)splits;
-        L.partial_stride = L.padded * width;
-        take(L.partial, splits > 1 || pieces > 1 ? (size_t)splits * L.partial_stride * 4 : 0);
+        take(L.partial, splits > 1 || pieces > 1 ? (size_t)(splits * tiles * kPartialTile) * sizeof(float4) : 0);
     }
     L.total = off;
     return L;
 }
 
 template <int MODE, bool LONG, typename T>
-cudaError_t launch_product_as(const CUtensorMap &ma, const CUtensorMap &ma2, const CUtensorMap &mb, const CUtensorMap &mb2, const ProductArgs &a, cudaStream_t st) {
+cudaError_t launch_product_as(const CUtensorMap &ma, const CUtensorMap &ma2, const CUtensorMap &mb, const CUtensorMap &mb2, const CUtensorMap &mo, const ProductArgs &a, cudaStream_t st) {
     cudaError_t e = cudaFuncSetAttribute(product_kernel<MODE, LONG, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
     if (e != cudaSuccess) return e;
     const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * a.splits;
     const int64_t pairs = sm_count() / 2;
-    return launch_after_smem(product_kernel<MODE, LONG, T>, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), dim3(kProductThreads), kProductSmem, st, ma, ma2, mb, mb2, a);
+    return launch_after_smem(product_kernel<MODE, LONG, T>, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), dim3(kProductThreads), kProductSmem, st, ma, ma2, mb, mb2, mo, a);
 }
 template <int MODE, typename T>
-cudaError_t launch_product(const CUtensorMap &ma, const CUtensorMap &ma2, const CUtensorMap &mb, const CUtensorMap &mb2, const ProductArgs &a, cudaStream_t st) {
+cudaError_t launch_product(const CUtensorMap &ma, const CUtensorMap &ma2, const CUtensorMap &mb, const CUtensorMap &mb2, const CUtensorMap &mo, const ProductArgs &a, cudaStream_t st) {
     if constexpr (MODE == kStats)
-        if (a.k_blocks > kPass) return launch_product_as<MODE, true, T>(ma, ma2, mb, mb2, a, st);
-    return launch_product_as<MODE, false, T>(ma, ma2, mb, mb2, a, st);
+        if (a.k_blocks > kPass) return launch_product_as<MODE, true, T>(ma, ma2, mb, mb2, mo, a, st);
+    return launch_product_as<MODE, false, T>(ma, ma2, mb, mb2, mo, a, st);
 }
 
 // Row tiles that share a column tile: as many as fit in about a third of the second-level cache.
@@ -831,7 +880,7 @@ cudaError_t forward(const XentArgs &x, cudaStream_t st) {
     a.n_parts = L.n_parts;
     a.picked = (float *)(ws + L.picked);
     a.status = x.status;
-    e = launch_product<kStats, T>(mx, mg, mw, mw, a, st);
+    e = launch_product<kStats, T>(mx, mg, mw, mw, mw, a, st);
     if (e != cudaSuccess) return e;
     CombineArgs c{};
     c.head = a.head;
@@ -859,12 +908,14 @@ cudaError_t backward(const XentArgs &x, cudaStream_t st) {
     const bool bf16 = x.dtype == 1;
     cudaError_t e = launch_rows(x, L, true, st);
     if (e != cudaSuccess) return e;
-    CUtensorMap mx, mxg, mw, gk, gm, wn, xn, xng;
+    CUtensorMap mx, mxg, mw, gk, gm, wn, xn, xng, go, xo, wo;
     // G as the rows' operand of dx (its vocabulary is the depth) and of dw (its vocabulary are the rows)
     if (!make_map(&mx, bf16, x.x, x.width, x.rows, x.x_stride, kHalf) || !make_map(&mxg, bf16, ws + L.x, x.width, L.padded, x.width, kHalf) ||
         !make_map(&mw, bf16, x.w, x.width, x.vocab, x.w_stride, kHalf) || !make_map(&gk, bf16, ws + L.g, L.piece, L.padded, L.piece, kHalf) ||
         !make_map(&gm, bf16, ws + L.g, L.piece, L.padded, L.piece, kK) || !make_map(&wn, bf16, x.w, x.width, x.vocab, x.w_stride, kK) ||
-        !make_map(&xn, bf16, x.x, x.width, x.rows, x.x_stride, kK) || !make_map(&xng, bf16, ws + L.x, x.width, L.padded, x.width, kK))
+        !make_map(&xn, bf16, x.x, x.width, x.rows, x.x_stride, kK) || !make_map(&xng, bf16, ws + L.x, x.width, L.padded, x.width, kK) ||
+        !make_map(&go, bf16, ws + L.g, L.piece, L.padded, L.piece, 32) || (x.dx && !make_map(&xo, bf16, x.dx, x.width, x.rows, x.width, 32)) ||
+        (x.dw && !make_map(&wo, bf16, x.dw, x.width, x.vocab, x.width, 32)))
         return cudaErrorInvalidValue;
     const int64_t pieces = (x.vocab + L.piece - 1) / L.piece;
     const bool direct = L.splits == 1 && pieces == 1;
@@ -888,9 +939,7 @@ cudaError_t backward(const XentArgs &x, cudaStream_t st) {
         g.k_blocks = (int)((x.width + kK - 1) / kK);
         g.splits = 1;
         g.group = group_of(x.width * 2, g.m_tiles);
-        g.out = ws + L.g;
-        g.out_stride = L.piece;
-        e = launch_product<kGrad, T>(mx, mxg, mw, mw, g, st);
+        e = launch_product<kGrad, T>(mx, mxg, mw, mw, go, g, st);
         if (e != cudaSuccess) return e;
         if (x.dx) {
             ProductArgs d = a;
@@ -901,10 +950,9 @@ cudaError_t backward(const XentArgs &x, cudaStream_t st) {
             d.group = row_tiles < 8 ? row_tiles : 8;
             d.out = x.dx;
             d.out_stride = x.width;
-            d.partial = direct ? nullptr : (float *)(ws + L.partial);
-            d.partial_stride = L.partial_stride;
+            d.partial = direct ? nullptr : (float4 *)(ws + L.partial);
             d.add = p > 0;
-            e = launch_product<kDx, T>(gk, gk, wn, wn, d, st);
+            e = launch_product<kDx, T>(gk, gk, wn, wn, xo, d, st);
             if (e != cudaSuccess) return e;
         }
         if (x.dw) {
@@ -913,9 +961,7 @@ cudaError_t backward(const XentArgs &x, cudaStream_t st) {
             d.n_tiles = width_tiles;
             d.splits = 1;
             d.group = d.m_tiles < 8 ? d.m_tiles : 8;
-            d.out = x.dw;
-            d.out_stride = x.width;
-            e = launch_product<kDw, T>(gm, gm, xn, xng, d, st);
+            e = launch_product<kDw, T>(gm, gm, xn, xng, wo, d, st);
             if (e != cudaSuccess) return e;
         }
     }
@@ -923,13 +969,12 @@ cudaError_t backward(const XentArgs &x, cudaStream_t st) {
         JoinArgs j{};
         j.head = a.head;
         j.row_of = a.row_of;
-        j.rows = x.rows;
         j.width = x.width;
-        j.partial = (const float *)(ws + L.partial);
-        j.stride = L.partial_stride;
+        j.partial = (const float4 *)(ws + L.partial);
+        j.n_tiles = width_tiles;
         j.splits = L.splits;
         j.dx = x.dx;
-        int64_t grid = (x.rows * (x.width / 8) + 255) / 256;
+        int64_t grid = (int64_t)row_tiles * width_tiles * 32;
         if (grid > sm_count() * 8) grid = sm_count() * 8;
         return launch_after(xent_join_kernel<T>, dim3((unsigned)grid), dim3(256), st, j);
     }
