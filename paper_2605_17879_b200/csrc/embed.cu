@@ -6,7 +6,7 @@
 // the order, and with it the result, a matter of chance, and would serialise on frequent tokens; so the positions are sorted
 // by token first (a stable radix sort), and runs of one token are summed.
 //   1. embed_sort_*: least significant digit first, kDigitBits at a time; a CTA ranks a tile of keys with warp matches and
-//      counters of its own, so equal keys keep their order.  One tile: all digits in one launch.  More: two launches per digit.
+//      counters of its own, so equal keys keep their order.  Short lists: all digits in one launch.  Others: two launches per digit.
 //   2. embed_sum_kernel: a warp takes a window of 32 sorted positions and a strip of columns, loads eight rows' vectors at a
 //      time and adds them run by run.  A run inside the window is a finished row.  One that crosses its borders leaves a
 //      partial sum: two places a window, in order, so the partial sums are again a sorted list, a sixteenth as long, to which
@@ -30,7 +30,6 @@ constexpr int kWindow = 32;
 constexpr int kSumThreads = 256;
 constexpr int kSumWarps = kSumThreads / 32;
 constexpr uint32_t kHole = 0x80000000u;      // a place without a partial sum; its key keeps the list sorted
-constexpr int kCols = 8;                     // columns a thread of the lookup copies
 
 __device__ __forceinline__ int64_t token_at(const void *tokens, int bits, int64_t i) {
     return bits == 64 ? __ldg(reinterpret_cast<const long long *>(tokens) + i) : (int64_t)__ldg(reinterpret_cast<const int *>(tokens) + i);
@@ -38,68 +37,49 @@ __device__ __forceinline__ int64_t token_at(const void *tokens, int bits, int64_
 
 // ---- lookup ----------------------------------------------------------------------------------------------------------
 
-// Eight columns of a row, those behind `left` as they are.
-template <typename T>
-__device__ __forceinline__ void load_cols(const T *p, int left, bool wide, float (&x)[kCols]) {
-    if (wide && left >= kCols) {
-        if constexpr (sizeof(T) == 4) {
+// A warp takes a token and a strip of its row; where rows are whole vectors of 16 bytes, all of a lane's loads (up to eight)
+// are in flight before the first is scaled and stored.
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a, int strips) {
+    constexpr int V = 16 / sizeof(T), kVectors = 8;
+    constexpr int kStrip = WIDE ? 32 * V * kVectors : 256;      // columns
+    pdl_wait();
+    const int lane = lane_id();
+    const int64_t work = a.n * strips, warps = (int64_t)gridDim.x * 8;
+    for (int64_t u = (int64_t)blockIdx.x * 8 + warp_id(); u < work; u += warps) {
+        int64_t i = u, strip = 0;
+        if (strips > 1) {
+            i = (u >> 31) ? u / strips : (int64_t)((uint32_t)u / (uint32_t)strips);
+            strip = u - i * strips;
+        }
+        const int64_t tok = token_at(a.tokens, a.token_bits, i);
+        const bool good = tok >= 0 && tok < a.rows;
+        if (!good && strip == 0 && lane == 0 && a.status) atomicOr(a.status, kStatIndex);
+        const T *from = reinterpret_cast<const T *>(a.table) + (good ? tok : 0) * a.stride;
+        T *to = reinterpret_cast<T *>(a.out) + i * a.width;
+        const float nan = __uint_as_float(0x7FC00000u);
+        const int64_t c0 = strip * kStrip + (WIDE ? lane * V : lane);
+        if constexpr (WIDE) {
+            Bytes16 r[kVectors];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float4 r = reinterpret_cast<const float4 *>(p)[h];
-                x[4 * h] = r.x, x[4 * h + 1] = r.y, x[4 * h + 2] = r.z, x[4 * h + 3] = r.w;
+            for (int q = 0; q < kVectors; ++q)
+                if (good && c0 + q * 32 * V < a.width) r[q] = *reinterpret_cast<const Bytes16 *>(from + c0 + q * 32 * V);
+#pragma unroll
+            for (int q = 0; q < kVectors; ++q) {
+                const int64_t c = c0 + q * 32 * V;
+                if (c >= a.width) break;
+                T *t = reinterpret_cast<T *>(&r[q]);
+#pragma unroll
+                for (int j = 0; j < V; ++j) t[j] = Conv<T>::down(good ? __fmul_rn(Conv<T>::up(t[j]), a.scale) : nan);
+                store16_once(to + c, r[q]);
             }
         } else {
-            const uint4 r = *reinterpret_cast<const uint4 *>(p);
-            const T *t = reinterpret_cast<const T *>(&r);
 #pragma unroll
-            for (int j = 0; j < kCols; ++j) x[j] = Conv<T>::up(t[j]);
+            for (int q = 0; q < 8; ++q) {
+                const int64_t c = c0 + q * 32;
+                if (c < a.width) to[c] = Conv<T>::down(good ? __fmul_rn(Conv<T>::up(from[c]), a.scale) : nan);
+            }
         }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < kCols; ++j) x[j] = j < left ? Conv<T>::up(p[j]) : 0.0f;
-}
-template <typename T>
-__device__ __forceinline__ void store_cols(T *p, int left, bool wide, const float (&x)[kCols]) {
-    if (wide && left >= kCols) {
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                reinterpret_cast<float4 *>(p)[h] = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
-        } else {
-            Bytes16 r;
-            T *t = reinterpret_cast<T *>(&r);
-#pragma unroll
-            for (int j = 0; j < kCols; ++j) t[j] = Conv<T>::down(x[j]);
-            *reinterpret_cast<Bytes16 *>(p) = r;
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < kCols; ++j)
-        if (j < left) p[j] = Conv<T>::down(x[j]);
-}
-
-template <typename T>
-__global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a, int groups, bool wide) {
-    pdl_wait();
-    const int64_t work = a.n * groups;
-    for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < work; w += (int64_t)gridDim.x * 256) {
-        const int64_t i = w / groups;
-        const int64_t col = (w - i * groups) * kCols;
-        const int64_t tok = token_at(a.tokens, a.token_bits, i);
-        const int left = (int)min((int64_t)kCols, a.width - col);
-        float x[kCols];
-        if (tok >= 0 && tok < a.rows) {
-            load_cols(reinterpret_cast<const T *>(a.table) + tok * a.stride + col, left, wide, x);
-#pragma unroll
-            for (int j = 0; j < kCols; ++j) x[j] = __fmul_rn(x[j], a.scale);
-        } else {
-#pragma unroll
-            for (int j = 0; j < kCols; ++j) x[j] = __uint_as_float(0x7FC00000u);
-            if (col == 0 && a.status) atomicOr(a.status, kStatIndex);
-        }
-        store_cols(reinterpret_cast<T *>(a.out) + i * a.width + col, left, wide, x);
     }
 }
 
@@ -242,45 +222,98 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_move_kernel(const Sor
         }
 }
 
-// One tile: every digit in turn by one CTA.
-__global__ void __launch_bounds__(kSortThreads) embed_sort_tile_kernel(const SortArgs s) {
-    __shared__ SortShared sh;
-    __shared__ uint32_t keys[kTile], places[kTile];
+// Short lists: every digit in turn by one CTA of 1 024 threads, kItems keys each, in shared memory.
+constexpr int kShortThreads = 1024, kShortWarps = kShortThreads / 32;
+struct ShortShared {
+    alignas(16) uint16_t count[kShortWarps][kDigits];
+    uint32_t base[kDigits];
+    uint32_t scan[kShortWarps];
+};
+template <int kItems>
+__global__ void __launch_bounds__(kShortThreads) embed_sort_short_kernel(const SortArgs s) {
+    extern __shared__ uint4 dynamic[];
+    ShortShared &sh = *reinterpret_cast<ShortShared *>(dynamic);
+    uint32_t *keys = reinterpret_cast<uint32_t *>(reinterpret_cast<uint8_t *>(dynamic) + sizeof(ShortShared)), *places = keys + kItems * kShortThreads;
     pdl_wait();
-    uint32_t key[kSortItems], pos[kSortItems], rank[kSortItems];
-    bool have[kSortItems];
-    load_tile(s, 0, key, pos, have);
+    const int lane = lane_id(), warp = warp_id();
+    const int at = warp * (32 * kItems) + lane;          // the thread's keys: at, at + 32, ...
+    const int n = (int)s.a.n;
+    uint32_t key[kItems], pos[kItems], rank[kItems];
+#pragma unroll
+    for (int r = 0; r < kItems; ++r) {
+        const int i = at + r * 32;
+        key[r] = i < n ? key_at(s.a, i) : 0;
+        pos[r] = i;
+    }
     for (int d = 0; d < s.digits; ++d) {
         const int shift = d * kDigitBits;
-        rank_tile(sh, key, have, shift, rank);
-        const uint32_t mine = warps_before(sh);
-        sh.base[threadIdx.x] = digits_before(sh, mine);
+        for (int i = threadIdx.x; i < kShortWarps * kDigits / 8; i += kShortThreads) reinterpret_cast<uint4 *>(&sh.count[0][0])[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kSortItems; ++r)
-            if (have[r]) {
+        for (int r = 0; r < kItems; ++r) {               // (as rank_tile)
+            const bool have = at + r * 32 < n;
+            const uint32_t digit = have ? (key[r] >> shift) & (kDigits - 1) : kDigits;
+            const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
+            const int first = __ffs(same) - 1;
+            uint32_t before = 0;
+            if (lane == first && have) {
+                before = sh.count[warp][digit];
+                sh.count[warp][digit] = (uint16_t)(before + __popc(same));
+            }
+            before = __shfl_sync(0xFFFFFFFFu, before, first);
+            rank[r] = before + __popc(same & ((1u << lane) - 1));
+            __syncwarp();
+        }
+        __syncthreads();
+        // numbers before each warp, then before each digit
+        uint32_t mine = 0;
+        if (threadIdx.x < kDigits) {
+#pragma unroll 8
+            for (int w = 0; w < kShortWarps; ++w) {
+                const uint32_t c = sh.count[w][threadIdx.x];
+                sh.count[w][threadIdx.x] = (uint16_t)mine;
+                mine += c;
+            }
+        }
+        uint32_t upto = mine;
+        for (int k = 1; k < 32; k <<= 1) {
+            const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, upto, k);
+            if (lane >= k) upto += y;
+        }
+        if (lane == 31) sh.scan[warp] = upto;
+        __syncthreads();
+        if (threadIdx.x < kDigits) sh.base[threadIdx.x] = upto - mine + __reduce_add_sync(0xFFFFFFFFu, lane < warp ? sh.scan[lane] : 0u);
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kItems; ++r)
+            if (at + r * 32 < n) {
                 const uint32_t digit = (key[r] >> shift) & (kDigits - 1);
-                const uint32_t to = sh.base[digit] + sh.count[warp_id()][digit] + rank[r];
+                const uint32_t to = sh.base[digit] + sh.count[warp][digit] + rank[r];
                 keys[to] = key[r];
                 places[to] = pos[r];
             }
         __syncthreads();
-        const int at = warp_id() * (32 * kSortItems) + lane_id();
 #pragma unroll
-        for (int r = 0; r < kSortItems; ++r)
-            if (have[r]) {
+        for (int r = 0; r < kItems; ++r)
+            if (at + r * 32 < n) {
                 key[r] = keys[at + r * 32];
                 pos[r] = places[at + r * 32];
             }
-        __syncthreads();
+        // (the next digit's counters are cleared, and its keys written, after barriers that follow these reads)
     }
-    const int at = warp_id() * (32 * kSortItems) + lane_id();
 #pragma unroll
-    for (int r = 0; r < kSortItems; ++r)
-        if (have[r]) {
+    for (int r = 0; r < kItems; ++r)
+        if (at + r * 32 < n) {
             s.out_key[at + r * 32] = key[r];
             s.out_pos[at + r * 32] = pos[r];
         }
+}
+
+template <int kItems>
+cudaError_t launch_short(const SortArgs &s, cudaStream_t st) {
+    constexpr int smem = (int)sizeof(ShortShared) + kItems * kShortThreads * 8;
+    const cudaError_t e = cudaFuncSetAttribute(embed_sort_short_kernel<kItems>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    return e != cudaSuccess ? e : launch_after_smem(embed_sort_short_kernel<kItems>, dim3(1), dim3(kShortThreads), smem, st, s);
 }
 
 // ---- sums ------------------------------------------------------------------------------------------------------------
@@ -362,8 +395,20 @@ __device__ __forceinline__ int64_t warp_lower_bound(const uint32_t *key, int64_t
     return lo;
 }
 
+// Zero bytes from p on (a whole number of elements, aligned to one); the warp together, vectors of 16 bytes in between.
+__device__ __forceinline__ void clear_stretch(uint8_t *p, int64_t bytes) {
+    const int64_t head = min(bytes, (int64_t)((16 - ((uintptr_t)p & 15)) & 15));
+    uint16_t *ends = reinterpret_cast<uint16_t *>(p);
+    for (int64_t i = lane_id(); i * 2 < head; i += 32) ends[i] = 0;
+    const int64_t vectors = (bytes - head) / 16;
+    uint4 *mid = reinterpret_cast<uint4 *>(p + head);
+    for (int64_t i = lane_id(); i < vectors; i += 32) mid[i] = make_uint4(0, 0, 0, 0);
+    const int64_t done = head + vectors * 16;
+    for (int64_t i = done / 2 + lane_id(); i * 2 < bytes; i += 32) ends[i] = 0;
+}
+
 // Zeros for the rows of the table without tokens, 32 rows a warp: the sorted keys say which those are.
-template <typename O, bool WIDE>
+template <typename O>
 __device__ __forceinline__ void clear_rows(const SumArgs &s, int64_t warp, int64_t warps) {
     O *table = reinterpret_cast<O *>(s.dtable);
     const uint32_t *key = s.list.key;
@@ -380,14 +425,12 @@ __device__ __forceinline__ void clear_rows(const SumArgs &s, int64_t warp, int64
         }
         const bool empty = mine < s.rows && !(lo < end && key[lo] == (uint32_t)mine);
         uint32_t rows = __ballot_sync(0xFFFFFFFFu, empty);
-        for (; rows; rows &= rows - 1) {
-            O *row = table + (first + __ffs(rows) - 1) * s.width;
-            if constexpr (WIDE) {
-                constexpr int V = 16 / sizeof(O);
-                for (int64_t c = lane_id() * V; c < s.width; c += 32 * V) *reinterpret_cast<uint4 *>(row + c) = make_uint4(0, 0, 0, 0);
-            } else {
-                for (int64_t c = lane_id(); c < s.width; c += 32) row[c] = Conv<O>::down(0.0f);
-            }
+        while (rows) {                                // runs of them are one stretch of memory each
+            const int at = __ffs(rows) - 1;
+            const int run = __ffs(~(rows >> at) | (at ? 1u << (32 - at) : 0u)) - 1;      // (ends at row 32)
+            const int count = run < 0 ? 32 : run;
+            clear_stretch(reinterpret_cast<uint8_t *>(table + (first + at) * s.width), (int64_t)count * s.width * sizeof(O));
+            rows = at + count >= 32 ? 0u : rows & ~((1u << (at + count)) - 1);
         }
     }
 }
@@ -467,7 +510,7 @@ __global__ void __launch_bounds__(kSumThreads, sizeof(T) == 4 ? 2 : 3) embed_sum
     const int64_t all = gridDim.x, b = blockIdx.x;
     const int64_t cleared = b * s.clear_blocks / all;
     if ((b + 1) * s.clear_blocks / all > cleared) {
-        clear_rows<O, WIDE>(s, cleared * kSumWarps + warp_id(), (int64_t)s.clear_blocks * kSumWarps);
+        clear_rows<O>(s, cleared * kSumWarps + warp_id(), (int64_t)s.clear_blocks * kSumWarps);
         return;
     }
     const int64_t work = (s.list.n + kWindow - 1) / kWindow * s.strips;
@@ -572,16 +615,20 @@ bool aligned(const void *p, size_t to) { return (uintptr_t)p % to == 0; }
 
 size_t embed_grad_workspace(int64_t n, int64_t rows, int64_t width) { return grad_layout(n, rows, width).total; }
 
-cudaError_t launch_embed(const EmbedArgs &a, int dtype, cudaStream_t st) {
-    const int64_t groups = (a.width + kCols - 1) / kCols;
-    const size_t b = dtype_bytes(dtype);
+template <typename T>
+static cudaError_t launch_embed_as(const EmbedArgs &a, cudaStream_t st) {
+    const size_t b = sizeof(T);
     const bool wide = aligned(a.table, 16) && aligned(a.out, 16) && (a.width * b) % 16 == 0 && (a.stride * b) % 16 == 0;
-    int64_t grid = (a.n * groups + 255) / 256;
-    const int64_t most = (int64_t)sm_count() * 16;
+    const int64_t strip = wide ? 32 * 16 / b * 8 : 256;
+    const int64_t strips = (a.width + strip - 1) / strip;
+    int64_t grid = (a.n * strips + 7) / 8;
+    const int64_t most = (int64_t)sm_count() * 32;
     if (grid > most) grid = most;
-    if (dtype == 0) return launch_after(embed_kernel<float>, dim3((unsigned)grid), dim3(256), st, a, (int)groups, wide);
-    if (dtype == 1) return launch_after(embed_kernel<__nv_bfloat16>, dim3((unsigned)grid), dim3(256), st, a, (int)groups, wide);
-    return launch_after(embed_kernel<__half>, dim3((unsigned)grid), dim3(256), st, a, (int)groups, wide);
+    return wide ? launch_after(embed_kernel<T, true>, dim3((unsigned)grid), dim3(256), st, a, (int)strips)
+                : launch_after(embed_kernel<T, false>, dim3((unsigned)grid), dim3(256), st, a, (int)strips);
+}
+cudaError_t launch_embed(const EmbedArgs &a, int dtype, cudaStream_t st) {
+    return dtype == 0 ? launch_embed_as<float>(a, st) : dtype == 1 ? launch_embed_as<__nv_bfloat16>(a, st) : launch_embed_as<__half>(a, st);
 }
 
 cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st) {
@@ -596,11 +643,11 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
     s.digits = (bits + kDigitBits - 1) / kDigitBits;
     int at = 0;      // which of the two orders holds the result
     cudaError_t e;
-    if (L.tiles <= 1) {
-        s.first = 1;
+    // one CTA sorts 8 192 keys in 14 us, the launches per digit that many more take 23
+    if (a.n <= 8 * kShortThreads) {
         s.out_key = (uint32_t *)(ws + L.key[0]);
         s.out_pos = (uint32_t *)(ws + L.pos[0]);
-        e = launch_after(embed_sort_tile_kernel, dim3(1), dim3(kSortThreads), st, s);
+        e = a.n <= kShortThreads ? launch_short<1>(s, st) : a.n <= 2 * kShortThreads ? launch_short<2>(s, st) : a.n <= 4 * kShortThreads ? launch_short<4>(s, st) : launch_short<8>(s, st);
         if (e != cudaSuccess) return e;
     } else {
         for (int d = 0; d < s.digits; ++d) {
