@@ -5,8 +5,9 @@
 //
 // A warp takes a block of 256 parameters, eight consecutive ones a lane: the largest loads there are (32 bytes a lane),
 // and a block's largest magnitude, which the 8-bit states' scale needs, is one shuffle reduction of values that are in
-// registers already.  CTAs take chunks of eight blocks in turn; a table gives the tensor of a chunk's first block, from there
-// a warp walks forward, so that tensors of any size and number share one launch.
+// registers already.  Tensors of any size and number share one launch: a table gives the tensor of every eighth block.
+#include <type_traits>
+
 #include "train_ops.h"
 
 namespace guard {
@@ -66,64 +67,71 @@ __device__ __forceinline__ float reciprocal(float x) {
     return y;
 }
 
-// Eight values of a lane; those behind `left` are zero.
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, int left, bool wide, float (&x)[8]) {
-    if (wide && left >= 8) {
-        if constexpr (sizeof(T) == 4) {
-            const Bytes32 r = load32_once(p);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(r.w[j]);
-        } else {
-            const Bytes16 r = load16_once(p);
-            const T *t = reinterpret_cast<const T *>(&r);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = Conv<T>::up(t[j]);
-        }
-        return;
+// A lane's eight values as they lie in memory: one vector of 16 or 32 bytes, loaded whole where a block is whole.
+template <typename T> struct Raw8 {
+    using Vector = typename std::conditional<sizeof(T) == 4, Bytes32, Bytes16>::type;
+    Vector v;
+    __device__ __forceinline__ void load(const T *p) {
+        if constexpr (sizeof(T) == 4) v = load32_once(p);
+        else v = load16_once(p);
     }
+    __device__ __forceinline__ void load_some(const T *p, int left) {       // those before `left`, the rest zero
+        T *t = reinterpret_cast<T *>(&v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = j < left ? Conv<T>::up(p[j]) : 0.0f;
-}
-template <typename T>
-__device__ __forceinline__ void store8(T *p, int left, bool wide, const float (&x)[8]) {
-    if (wide && left >= 8) {
-        if constexpr (sizeof(T) == 4) {
-            Bytes32 r;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) r.w[j] = __float_as_uint(x[j]);
-            store32_once(p, r);
-        } else {
-            Bytes16 r;
-            T *t = reinterpret_cast<T *>(&r);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] = Conv<T>::down(x[j]);
-            store16_once(p, r);
-        }
-        return;
+        for (int j = 0; j < 8; ++j) t[j] = j < left ? p[j] : Conv<T>::down(0.0f);
     }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        const T *t = reinterpret_cast<const T *>(&v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j < left) p[j] = Conv<T>::down(x[j]);
-}
-// Eight 8-bit values of a lane, times their scale (a power of two: exact).
-__device__ __forceinline__ void load8_e4m3(const uint8_t *p, int left, float scale, float (&x)[8]) {
-    uint32_t w[2] = {0, 0};
-    if (left >= 8) {
-        asm volatile("ld.global.L1::no_allocate.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+        for (int j = 0; j < 8; ++j) x[j] = Conv<T>::up(t[j]);
+    }
+};
+template <bool FAST, typename T>
+__device__ __forceinline__ void store8(T *p, int left, const float (&x)[8]) {
+    if constexpr (FAST) {
+        typename Raw8<T>::Vector r;
+        T *t = reinterpret_cast<T *>(&r);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = Conv<T>::down(x[j]);
+        if constexpr (sizeof(T) == 4) store32_once(p, r);
+        else store16_once(p, r);
     } else {
-        for (int j = 0; j < left; ++j) w[j >> 2] |= (uint32_t)p[j] << (8 * (j & 3));
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < left) p[j] = Conv<T>::down(x[j]);
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) from_e4m3x2(w[j >> 1] >> (16 * (j & 1)), x[2 * j], x[2 * j + 1]);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = __fmul_rn(x[j], scale);
 }
+// A lane's eight values of a state: float32, or e4m3 with the block's scale (a power of two: the product is exact).
+template <int BITS> struct RawState : Raw8<float> {
+    __device__ __forceinline__ void load(const void *p, const float *, int64_t flat, int64_t) { Raw8<float>::load(reinterpret_cast<const float *>(p) + flat); }
+    __device__ __forceinline__ void load_some(const void *p, const float *, int64_t flat, int64_t, int left) {
+        Raw8<float>::load_some(reinterpret_cast<const float *>(p) + flat, left);
+    }
+};
+template <> struct RawState<8> {
+    uint32_t w[2];
+    float scale;
+    __device__ __forceinline__ void load(const void *p, const float *scales, int64_t flat, int64_t block) {
+        asm volatile("ld.global.L1::no_allocate.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(reinterpret_cast<const uint8_t *>(p) + flat));
+        scale = scales[block];
+    }
+    __device__ __forceinline__ void load_some(const void *p, const float *scales, int64_t flat, int64_t block, int left) {
+        w[0] = w[1] = 0;
+        for (int j = 0; j < left; ++j) w[j >> 2] |= (uint32_t) reinterpret_cast<const uint8_t *>(p)[flat + j] << (8 * (j & 3));
+        scale = scales[block];
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) from_e4m3x2(w[j >> 1] >> (16 * (j & 1)), x[2 * j], x[2 * j + 1]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = __fmul_rn(x[j], scale);
+    }
+};
 // Stores x as 8-bit values of the block's scale, which it returns: the power of two by which the block's largest magnitude
 // comes to lie in (224, 448], 448 being e4m3's largest value.  Powers of two keep the grid of values as it is when the
 // scale changes, so a value moves only by what the update adds to it: with the largest magnitude itself as the scale, every
 // step would round every value anew, and the noise of that adds up over the 1 / (1 - beta2) steps that a mean remembers.
-template <bool LEAST>
+template <bool FAST, bool LEAST>
 __device__ __forceinline__ float store8_e4m3(uint8_t *p, int left, const float (&x)[8], const uint32_t (&bits)[8]) {
     uint32_t top = 0;                          // magnitudes order as their bits do
 #pragma unroll
@@ -154,7 +162,7 @@ __device__ __forceinline__ float store8_e4m3(uint8_t *p, int left, const float (
     uint32_t w[2] = {0, 0};
 #pragma unroll
     for (int j = 0; j < 8; j += 2) w[j >> 2] |= to_e4m3x2(y[j], y[j + 1]) << (16 * ((j >> 1) & 1));
-    if (left >= 8) {
+    if constexpr (FAST) {
         asm volatile("st.global.L1::no_allocate.v2.b32 [%2], {%0,%1};" ::"r"(w[0]), "r"(w[1]), "l"(p) : "memory");
     } else {
         for (int j = 0; j < left; ++j) p[j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
@@ -162,79 +170,138 @@ __device__ __forceinline__ float store8_e4m3(uint8_t *p, int left, const float (
     return __uint_as_float(e << 23);
 }
 
-// Four CTAs an SM (64 registers), and as many in the grid: with 74 registers three fit, and the fourth ran alone after them.
-constexpr int kResident = 4;
+// CTAs an SM, and as many in the grid: 128 registers hold the next block's values without spilling.  404 M parameters with
+// 8-bit states take 1 218 us so (5.3 TB/s), 1 355 with four CTAs of 64 registers and nothing on its way.
+constexpr int kResident = 2;
+
+struct Rates { float rate, grow, lr, grad_scale; uint32_t key; };
+
+// What a lane reads of a block.
+template <typename G, int BITS> struct Block {
+    Raw8<float> p;
+    Raw8<G> g;
+    RawState<BITS> m, v;
+    __device__ __forceinline__ void load(const AdamwArgs &a, const AdamwTensor &T, int64_t b) {
+        const int64_t at = (b - T.first) * kAdamwBlock + lane_id() * 8, flat = b * kAdamwBlock + lane_id() * 8;
+        p.load(T.param + at);
+        g.load(reinterpret_cast<const G *>(T.grad) + at);
+        m.load(a.m, a.m_scale, flat, b);
+        v.load(a.v, a.v_scale, flat, b);
+    }
+    __device__ __forceinline__ void load_some(const AdamwArgs &a, const AdamwTensor &T, int64_t b, int left) {
+        const int64_t at = (b - T.first) * kAdamwBlock + lane_id() * 8, flat = b * kAdamwBlock + lane_id() * 8;
+        p.load_some(T.param + at, left);
+        g.load_some(reinterpret_cast<const G *>(T.grad) + at, left);
+        m.load_some(a.m, a.m_scale, flat, b, left);
+        v.load_some(a.v, a.v_scale, flat, b, left);
+    }
+};
+
+// Updates a block and stores it; FAST: all 256 parameters are there and every pointer is aligned to a lane's eight.
+// param, copy (or NULL): the lane's first.
+template <bool FAST, typename G, typename Cp, int BITS>
+__device__ __forceinline__ void update_block(const AdamwArgs &a, const Block<G, BITS> &in, float *param, Cp *copy, float decay, int64_t b, int left, const Rates &c) {
+    const int64_t flat = b * kAdamwBlock + lane_id() * 8;             // in the states
+    float p[8], g[8], m[8], v[8];
+    in.p.get(p);
+    in.g.get(g);
+    in.m.get(m);
+    in.v.get(v);
+    const float keep = (float)(1.0 - (double)c.lr * decay);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float gj = __fmul_rn(g[j], c.grad_scale);
+        m[j] = __fadd_rn(__fmul_rn(m[j], a.beta1), __fmul_rn(gj, a.rest1));
+        v[j] = __fadd_rn(__fmul_rn(v[j], a.beta2), __fmul_rn(__fmul_rn(gj, gj), a.rest2));
+        // root and reciprocal are good to 2^-23 (second moments below 2^-126 count as zero here)
+        const float den = __fmaf_rn(root(v[j]), c.grow, a.eps);
+        p[j] = __fmaf_rn(p[j], keep, -__fmul_rn(c.rate, __fmul_rn(m[j], reciprocal(den))));
+    }
+    store8<FAST>(param, left, p);
+    if (copy) store8<FAST>(copy, left, p);
+    if constexpr (BITS == 32) {
+        store8<FAST>(reinterpret_cast<float *>(a.m) + flat, left, m);
+        store8<FAST>(reinterpret_cast<float *>(a.v) + flat, left, v);
+    } else {
+        uint32_t lo[8], hi[8];
+        // (eight positions from a multiple of eight on differ in the low word alone)
+        const uint32_t place = (uint32_t)flat + (uint32_t)(flat >> 32) * 0x85EBCA6Bu;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (!FAST && j >= left) m[j] = v[j] = 0.0f;
+            const uint32_t h = dither(place + j, c.key);
+            lo[j] = (h << 4) & 0xFFFF0u;
+            hi[j] = (h >> 12) & 0xFFFF0u;
+        }
+        const float ms = store8_e4m3<FAST, false>(reinterpret_cast<uint8_t *>(a.m) + flat, left, m, lo);
+        const float vs = store8_e4m3<FAST, true>(reinterpret_cast<uint8_t *>(a.v) + flat, left, v, hi);
+        if (lane_id() == 0) {
+            a.m_scale[b] = ms;
+            a.v_scale[b] = vs;
+        }
+    }
+}
+// (Out of line: what the ends of tensors need does not weigh on the registers of the common case.)
+template <typename G, typename Cp, int BITS>
+__device__ __noinline__ void update_end(const AdamwArgs &a, const AdamwTensor &T, int64_t b, const Rates &c) {
+    const int64_t at = (b - T.first) * kAdamwBlock + lane_id() * 8;
+    const int left = (int)max((int64_t)0, min((int64_t)8, T.count - at));
+    Block<G, BITS> in;
+    in.load_some(a, T, b, left);
+    update_block<false, G, Cp, BITS>(a, in, T.param + at, T.copy ? reinterpret_cast<Cp *>(T.copy) + at : nullptr, T.decay, b, left, c);
+}
 
 template <typename G, typename Cp, int BITS>
-__global__ void __launch_bounds__(kThreads, kResident) adamw_kernel(const AdamwArgs a) {
-    __shared__ float s_rate, s_grow, s_lr;
+__global__ void __launch_bounds__(kThreads, kResident) adamw_kernel(const __grid_constant__ AdamwArgs a) {
+    __shared__ Rates s_rates;
     pdl_wait();
     const int64_t t = a.counter->step + 1;
+    // a warp takes every (warps of the grid)-th block: looks the first one's tensor up, then walks along.  The next block's
+    // values are on their way while one is updated.
+    const int64_t step = (int64_t)gridDim.x * (kThreads / 32);
+    int64_t b = (int64_t)blockIdx.x * (kThreads / 32) + warp_id();
+    int k = b < a.blocks ? (int)a.tensor_of[b / kAdamwChunk] : 0;
+    AdamwTensor T = a.tensors[k];
+    int64_t end = k + 1 < a.n ? a.tensors[k + 1].first : INT64_MAX;
+    Block<G, BITS> next;
+    auto fetch = [&](int64_t i) {           // block i's tensor and, where it is whole, its values
+        if (i >= a.blocks) return false;
+        if (i >= end) {
+            do {
+                ++k;
+                end = k + 1 < a.n ? a.tensors[k + 1].first : INT64_MAX;
+            } while (i >= end);
+            T = a.tensors[k];
+        }
+        if (!T.wide || (i - T.first + 1) * kAdamwBlock > T.count) return false;
+        next.load(a, T, i);
+        return true;
+    };
+    bool whole = fetch(b);
     if (threadIdx.x == 0) {
         const double lr = a.d_lr ? (double)*a.d_lr : a.lr;
-        s_rate = (float)(lr / (1.0 - power(a.dbeta1, t)));
-        s_grow = (float)(1.0 / sqrt(1.0 - power(a.dbeta2, t)));
-        s_lr = (float)lr;
+        s_rates.rate = (float)(lr / (1.0 - power(a.dbeta1, t)));
+        s_rates.grow = (float)(1.0 / sqrt(1.0 - power(a.dbeta2, t)));
+        s_rates.lr = (float)lr;
+        s_rates.grad_scale = a.grad_scale ? *a.grad_scale : 1.0f;
+        s_rates.key = a.seed + (uint32_t)t * 0x9E3779B9u;
     }
-    const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
-    const uint32_t key = a.seed + (uint32_t)t * 0x9E3779B9u;
     __syncthreads();
-    const float rate = s_rate, grow = s_grow, lr = s_lr;
-    const int lane = lane_id(), warp = warp_id();
-    const int64_t chunks = (a.blocks + kAdamwChunk - 1) / kAdamwChunk;
-    for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        int k = (int)a.tensor_of[c];
-        const int64_t end = min(a.blocks, (c + 1) * kAdamwChunk);
-        for (int64_t b = c * kAdamwChunk + warp; b < end; b += kThreads / 32) {
-            while (k + 1 < a.n && a.tensors[k + 1].first <= b) ++k;
-            const AdamwTensor T = a.tensors[k];
-            const int64_t at = (b - T.first) * kAdamwBlock + lane * 8;   // in the tensor
-            const int64_t flat = b * kAdamwBlock + lane * 8;             // in the states
-            const int left = (int)max((int64_t)0, min((int64_t)8, T.count - at));
-            const bool wide = T.wide != 0;
-            float p[8], g[8], m[8], v[8];
-            load8(T.param + at, left, wide, p);
-            load8(reinterpret_cast<const G *>(T.grad) + at, left, wide, g);
-            if constexpr (BITS == 32) {
-                load8(reinterpret_cast<const float *>(a.m) + flat, left, true, m);
-                load8(reinterpret_cast<const float *>(a.v) + flat, left, true, v);
-            } else {
-                load8_e4m3(reinterpret_cast<const uint8_t *>(a.m) + flat, left, a.m_scale[b], m);
-                load8_e4m3(reinterpret_cast<const uint8_t *>(a.v) + flat, left, a.v_scale[b], v);
-            }
-            const float keep = (float)(1.0 - (double)lr * T.decay);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float gj = __fmul_rn(g[j], gs);
-                m[j] = __fadd_rn(__fmul_rn(m[j], a.beta1), __fmul_rn(gj, a.rest1));
-                v[j] = __fadd_rn(__fmul_rn(v[j], a.beta2), __fmul_rn(__fmul_rn(gj, gj), a.rest2));
-                // root and reciprocal are good to 2^-23 (second moments below 2^-126 count as zero here)
-                const float den = __fmaf_rn(root(v[j]), grow, a.eps);
-                p[j] = __fmaf_rn(p[j], keep, -__fmul_rn(rate, __fmul_rn(m[j], reciprocal(den))));
-            }
-            store8(T.param + at, left, wide, p);
-            if (T.copy) store8(reinterpret_cast<Cp *>(T.copy) + at, left, wide, p);
-            if constexpr (BITS == 32) {
-                store8(reinterpret_cast<float *>(a.m) + flat, left, true, m);
-                store8(reinterpret_cast<float *>(a.v) + flat, left, true, v);
-            } else {
-                uint32_t lo[8], hi[8];
-                // (eight positions from a multiple of eight on differ in the low word alone)
-                const uint32_t place = (uint32_t)flat + (uint32_t)(flat >> 32) * 0x85EBCA6Bu;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (j >= left) m[j] = v[j] = 0.0f;
-                    const uint32_t h = dither(place + j, key);
-                    lo[j] = (h << 4) & 0xFFFF0u;
-                    hi[j] = (h >> 12) & 0xFFFF0u;
-                }
-                const float ms = store8_e4m3<false>(reinterpret_cast<uint8_t *>(a.m) + flat, left, m, lo);
-                const float vs = store8_e4m3<true>(reinterpret_cast<uint8_t *>(a.v) + flat, left, v, hi);
-                if (lane == 0) {
-                    a.m_scale[b] = ms;
-                    a.v_scale[b] = vs;
-                }
-            }
+    const Rates c = s_rates;
+    while (b < a.blocks) {
+        if (whole) {
+            const Block<G, BITS> now = next;
+            const int64_t at = (b - T.first) * kAdamwBlock + lane_id() * 8, done = b;
+            float *param = T.param + at;
+            Cp *copy = T.copy ? reinterpret_cast<Cp *>(T.copy) + at : nullptr;
+            const float decay = T.decay;
+            b += step;
+            whole = fetch(b);
+            update_block<true, G, Cp, BITS>(a, now, param, copy, decay, done, 8, c);
+        } else {
+            update_end<G, Cp, BITS>(a, a.tensors[k], b, s_rates);
+            b += step;
+            whole = fetch(b);
         }
     }
     // the last CTA to get here counts the step: every other one has read the counter before
@@ -262,9 +329,8 @@ cudaError_t launch_copy(const AdamwArgs &a, int copy, int bits, int grid, cudaSt
 }  // namespace
 
 cudaError_t launch_adamw(const AdamwArgs &a, int grad_dtype, int copy_dtype, int state_bits, cudaStream_t st) {
-    const int64_t chunks = (a.blocks + kAdamwChunk - 1) / kAdamwChunk;
     int64_t grid = (int64_t)sm_count() * kResident;
-    if (grid > chunks) grid = chunks;
+    if (grid > (a.blocks + kThreads / 32 - 1) / (kThreads / 32)) grid = (a.blocks + kThreads / 32 - 1) / (kThreads / 32);      // (a block for each warp)
     if (grid < 1) grid = 1;
     return grad_dtype == 2   ? launch_copy<__half>(a, copy_dtype, state_bits, (int)grid, st)
            : grad_dtype == 1 ? launch_copy<__nv_bfloat16>(a, copy_dtype, state_bits, (int)grid, st)

@@ -10,7 +10,7 @@
 //   2. embed_sum_kernel: a warp takes a window of 32 sorted positions and a strip of columns, loads eight rows' vectors at a
 //      time and adds them run by run.  A run inside the window is a finished row.  One that crosses its borders leaves a
 //      partial sum: two places a window, in order, so the partial sums are again a sorted list, a sixteenth as long, to which
-//      the same is applied until one window is left (by embed_finish_kernel once the list is short).  So a token that occurs once costs one read and one write, one that
+//      the same is applied until the list is short; embed_finish_kernel then adds each token's places.  So a token that occurs once costs one read and one write, one that
 //      fills the batch is summed by as many warps as there are windows, and nothing depends on how frequent tokens are.
 //      The first of these launches also writes zeros to the rows whose token is not in the list.
 // The grouping of a sum depends on the positions alone.
@@ -330,7 +330,6 @@ struct List {
 
 struct SumArgs {
     List list;                   // sorted keys (kHole: nothing there)
-    float *spare;                // embed_finish_kernel: a place for a third list
     int64_t rows, width;
     float scale;
     int accumulate;
@@ -435,6 +434,22 @@ __device__ __forceinline__ void clear_rows(const SumArgs &s, int64_t warp, int64
     }
 }
 
+// A row's sum is complete: scaled, added to what the table holds where that is wanted, and stored.
+template <typename O, bool WIDE, int V>
+__device__ __forceinline__ void finish_row(const SumArgs &s, uint32_t row, int64_t strip, float (&sum)[V]) {
+    O *out = reinterpret_cast<O *>(s.dtable) + (int64_t)row * s.width;
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[e] = __fmul_rn(sum[e], s.scale);
+    if (s.accumulate) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const int64_t c = column<WIDE, V>(strip, e);
+            if (c < s.width) sum[e] = __fadd_rn(Conv<O>::up(out[c]), sum[e]);
+        }
+    }
+    store_strip<O, WIDE, V>(out, strip, s.width, sum);
+}
+
 // One warp, one window of the list, one strip of columns.  T: the list's rows (the gradient's type, or float32 for partial
 // sums); O: the table's.
 template <typename T, typename O, bool WIDE>
@@ -480,18 +495,7 @@ __device__ __forceinline__ void sum_window(const SumArgs &s, const List &l, int6
                         full1 |= !from_before;
                         store_strip<float, WIDE, V>(l.next + (2 * w + (from_before ? 0 : 1)) * s.width, strip, s.width, sum);
                     } else {
-                        const uint32_t row = __shfl_sync(0xFFFFFFFFu, key, b + j);
-                        O *out = reinterpret_cast<O *>(s.dtable) + (int64_t)row * s.width;
-#pragma unroll
-                        for (int e = 0; e < V; ++e) sum[e] = __fmul_rn(sum[e], s.scale);
-                        if (s.accumulate) {
-#pragma unroll
-                            for (int e = 0; e < V; ++e) {
-                                const int64_t c = column<WIDE, V>(strip, e);
-                                if (c < s.width) sum[e] = __fadd_rn(Conv<O>::up(out[c]), sum[e]);
-                            }
-                        }
-                        store_strip<O, WIDE, V>(out, strip, s.width, sum);
+                        finish_row<O, WIDE, V>(s, __shfl_sync(0xFFFFFFFFu, key, b + j), strip, sum);
                     }
                 }
 #pragma unroll
@@ -522,32 +526,58 @@ __global__ void __launch_bounds__(kSumThreads, sizeof(T) == 4 ? 2 : 3) embed_sum
     }
 }
 
-// The last lists of partial sums, a CTA per strip: it keeps the keys of the lists that it makes to itself.
-constexpr int kFinish = 512;
+// The last list of partial sums, a CTA per strip of 128 columns: a warp per token adds its places in order.
+constexpr int kFinish = 512, kFinishThreads = 512;
 template <typename O, bool WIDE>
-__global__ void __launch_bounds__(kSumThreads, 2) embed_finish_kernel(const SumArgs s) {
-    __shared__ uint32_t keys[2][2 * kFinish / kWindow];
+__global__ void __launch_bounds__(kFinishThreads) embed_finish_kernel(const SumArgs s) {
+    constexpr int V = 4, kBatch = 8;
+    __shared__ uint32_t keys[kFinish];
+    __shared__ uint16_t runs[kFinish];
+    __shared__ int count;
+    if (threadIdx.x == 0) count = 0;
     pdl_wait();
-    List l = s.list;
-    float *spare = s.spare;
-    for (int level = 0;; ++level) {
-        const int64_t windows = (l.n + kWindow - 1) / kWindow;
-        l.next_key = windows > 1 ? keys[level & 1] : nullptr;
-        for (int64_t w = warp_id(); w < windows; w += kSumWarps) sum_window<float, O, WIDE>(s, l, w, blockIdx.x);
-        if (windows <= 1) return;
-        __syncthreads();
-        l.n = 2 * windows;
-        l.key = l.next_key;
-        float *was = (float *)l.from;
-        l.from = l.next;
-        l.next = level == 0 ? spare : was;
+    const int n = (int)s.list.n, i = threadIdx.x;
+    keys[i] = i < n ? s.list.key[i] : 0xFFFFFFFFu;
+    __syncthreads();
+    // a token's first place that holds something (in any order: every token is added by itself)
+    const uint32_t key = keys[i];
+    if (!(key & kHole) && key < (uint32_t)s.rows) {
+        int j = i - 1;
+        while (j >= 0 && keys[j] == (key | kHole)) --j;
+        if (j < 0 || keys[j] != key) runs[atomicAdd(&count, 1)] = (uint16_t)i;
+    }
+    __syncthreads();
+    const int64_t strip = blockIdx.x;
+    const float *from = reinterpret_cast<const float *>(s.list.from);
+    for (int r = warp_id(); r < count; r += kFinishThreads / 32) {
+        int at = runs[r];
+        const uint32_t row = keys[at];
+        float sum[V] = {};
+        while (at < n && (keys[at] & ~kHole) == row) {
+            float x[kBatch][V];
+            uint32_t have = 0;
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j)
+                if (at + j < n && keys[at + j] == row) {
+                    have |= 1u << j;
+                    load_strip<float, WIDE, V>(from + (int64_t)(at + j) * s.list.stride, strip, s.width, x[j]);
+                }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j)
+                if ((have >> j) & 1) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) sum[e] = __fadd_rn(sum[e], x[j][e]);
+                }
+            at += kBatch;
+        }
+        finish_row<O, WIDE, V>(s, row, strip, sum);
     }
 }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct GradLayout {
-    size_t key[2], pos[2], counts, next_key[3], next[3], total;
+    size_t key[2], pos[2], counts, next_key[2], next[2], total;
     int64_t tiles;
 };
 // Places of the list that a list of n leaves (0: none).
@@ -561,9 +591,9 @@ GradLayout grad_layout(int64_t n, int64_t rows, int64_t width) {
         L.pos[i] = off, off = up256(off + (size_t)n * 4);
     }
     L.counts = off, off = up256(off + (size_t)L.tiles * kDigits * 4);
-    // lists of partial sums: each is read while the next one is written
+    // two lists of partial sums, used in turn
     int64_t m = next_length(n);
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < 2; ++i) {
         L.next_key[i] = off, off = up256(off + (size_t)m * 4);
         L.next[i] = off, off = up256(off + (size_t)m * width * 4);
         m = next_length(m);
@@ -593,14 +623,13 @@ cudaError_t launch_sum(SumArgs s, bool first, bool wide, cudaStream_t st) {
 template <typename T>
 cudaError_t launch_sums(SumArgs s, const GradLayout &L, char *ws, bool wide, cudaStream_t st) {
     for (int level = 0;; ++level) {
-        const int to = level % 3;       // three lists in turn: the first two lengths are the largest
+        const int to = level & 1;
         const int64_t next = next_length(s.list.n);
         s.list.next_key = next ? (uint32_t *)(ws + L.next_key[to]) : nullptr;
         s.list.next = next ? (float *)(ws + L.next[to]) : nullptr;
         cudaError_t e;
         if (level > 0 && s.list.n <= kFinish) {
-            s.spare = (float *)(ws + L.next[(to + 1) % 3]);
-            const dim3 grid((unsigned)((s.width + 127) / 128)), block(kSumThreads);
+            const dim3 grid((unsigned)((s.width + 127) / 128)), block(kFinishThreads);
             return wide ? launch_after(embed_finish_kernel<T, true>, grid, block, st, s) : launch_after(embed_finish_kernel<T, false>, grid, block, st, s);
         }
         e = level == 0 ? launch_sum<T, T>(s, true, wide, st) : launch_sum<float, T>(s, false, wide, st);

@@ -70,7 +70,7 @@ struct AdamwCounter {       // at the start of the workspace
 };
 struct AdamwArgs {
     const AdamwTensor *tensors;
-    const uint32_t *tensor_of;   // [chunks] tensor of a chunk's first block
+    const uint32_t *tensor_of;   // tensor of every kAdamwChunk-th block
     AdamwCounter *counter;
     int64_t blocks;
     int n;
@@ -82,7 +82,7 @@ struct AdamwArgs {
     uint32_t seed;
 };
 constexpr int kAdamwBlock = 256;
-constexpr int kAdamwChunk = 8;     // blocks that a CTA takes at a time: one a warp
+constexpr int kAdamwChunk = 8;     // blocks to an entry of the table that finds a block's tensor
 cudaError_t launch_adamw(const AdamwArgs &a, int grad_dtype, int copy_dtype, int state_bits, cudaStream_t st);
 
 struct EmbedArgs {
