@@ -1,5 +1,6 @@
 // C entries of the training-step operators: argument checks on the host, then the launches.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -22,12 +23,18 @@ int call_error(int code, const char *fmt, ...) {
 }
 
 int sm_count() {
+    static std::atomic<int> known[64];
     int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
-        (void)cudaGetLastError();
-        return 148;
+    if (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64) {
+        n = known[dev].load(std::memory_order_relaxed);
+        if (n > 0) return n;
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n >= 2) {
+            known[dev].store(n, std::memory_order_relaxed);
+            return n;
+        }
     }
-    return n;
+    (void)cudaGetLastError();
+    return 148;
 }
 
 }  // namespace guard

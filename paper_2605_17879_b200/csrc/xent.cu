@@ -22,6 +22,7 @@
 // hold (NaN among it) reaches nothing.
 #include <cudaTypedefs.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "tcgen05.cuh"
@@ -43,7 +44,7 @@ constexpr int kBox = 32 * 128;                // bytes of what a warp stores at 
 constexpr int kProductSmem = kStages * kStage + kEpilogueWarps * kBox + 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 
-enum Mode { kStats, kGrad, kDx, kDw };
+enum Mode { kStats, kGrad, kBack };      // kBack: dx and dw in one launch
 
 struct Header {         // at the start of the workspace, written by xent_rows_kernel
     int32_t count;      // rows that take part
@@ -52,13 +53,15 @@ struct Header {         // at the start of the workspace, written by xent_rows_k
     float inverse;      // what a gradient from G is multiplied by: unit / scale
 };
 
+struct Maps { CUtensorMap a, a2, b, b2, b3, out, out2; };   // of the operands and results (see where each is used)
+
 struct ProductArgs {
     const Header *head;    // or NULL: all rows
     int rows;              // N
-    int64_t vocab;
-    int m_tiles, n_tiles, k_blocks;   // of the whole problem (the rows' part: at most)
-    int splits;            // of the depth (kDx)
+    int64_t vocab, width;
+    int m_tiles, n_tiles, k_blocks;   // kStats, kGrad: of the logits; kBack: of dx (m_tiles 0: not wanted)
     int group;             // row tiles that share column tiles while those are in the second-level cache
+    int dw_tiles, dw_group;           // row tiles of dw (0: not wanted)
     int64_t v0;            // first vocabulary entry of the piece
     const int32_t *target; // [rows] vocabulary index or -1, by (gathered) row
     const void *raw_target;   // without a header: int32 or int64 as the caller gave them
@@ -67,12 +70,12 @@ struct ProductArgs {
     float2 *parts;         // [rows][n_parts] largest value and sum
     int n_parts;
     float *picked;         // [rows] logit of the target
-    void *out;             // kDx: dx, where gathered rows are scattered
-    int64_t out_stride;
-    const int32_t *row_of; // gathered row -> row (dx)
-    float4 *partial;       // kDx: partial sums by tile and split, as threads hold them (see partial_at)
+    void *dx;              // where gathered rows are scattered
+    int64_t dx_stride;
+    const int32_t *row_of; // gathered row -> row
+    float4 *partial;       // or NULL: partial sums of dx by tile and split, as threads hold them (see partial_at)
+    int max_units, max_splits;        // places in it, and splits that the depth allows
     int add;               // add to partial
-    int64_t width;
     uint32_t *status;
 };
 
@@ -103,21 +106,82 @@ __device__ __forceinline__ bool wait_for(ProductShared &s, uint64_t *bar, uint32
     return true;
 }
 
-struct Tile { int m, n, split; };
+// Parts into which the depth of dx is split: as many as keep every pair of CTAs busy and have a place.
+__device__ __forceinline__ int dx_splits(int tiles, int max_units, int max_splits) { return tiles > 0 ? max(1, min(max_units / tiles, max_splits)) : 1; }
 
-// The t-th tile: groups of row tiles, column tile after column tile within a group.
-__device__ __forceinline__ Tile tile_at(int t, int m_tiles, int n_tiles, int group, int splits) {
-    Tile r;
-    r.split = t % splits;
-    t /= splits;
-    const int per = group * n_tiles;
-    const int g = t / per, first = g * group;
-    const int high = min(group, m_tiles - first);
-    const int in = t - g * per;
-    r.m = first + in % high;
-    r.n = in / high;
-    return r;
-}
+// One accumulation: a tile and the stages of depth that it takes.
+struct Unit {
+    bool dw;
+    int m, n, k0, k1;
+    int64_t place;         // of its partial sum
+};
+
+// The units of one pair of CTAs, in order; every warp that has a part in them goes through the same ones.
+struct Work {
+    int pairs, pair, m_tiles, n_tiles, k_blocks, group, splits, units;
+    int dw_m, dw_group, dw_k, dw_units, early, early_each, rest;     // kBack
+    int i, phase;
+
+    template <int MODE>
+    __device__ __forceinline__ void begin(const ProductArgs &a, int rows) {
+        pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
+        n_tiles = a.n_tiles, k_blocks = a.k_blocks, group = a.group;
+        m_tiles = MODE == kBack && a.m_tiles == 0 ? 0 : (rows + kM - 1) / kM;
+        splits = MODE == kBack && a.partial ? dx_splits(m_tiles * n_tiles, a.max_units, a.max_splits) : 1;
+        units = m_tiles * n_tiles * splits;
+        dw_units = 0;
+        i = phase = 0;
+        if constexpr (MODE == kBack) {
+            dw_m = a.dw_tiles, dw_group = a.dw_group;
+            dw_k = (rows + kK - 1) / kK;
+            dw_units = dw_m * n_tiles;
+            // units of dx are few and long: pairs that got one less than others take tiles of dw for it first
+            rest = units % pairs;
+            early_each = rest ? k_blocks / splits / max(dw_k, 1) : 0;
+            early = (int)min((int64_t)dw_units, (int64_t)(pairs - rest) * early_each);
+        }
+    }
+    // The t-th tile: groups of row tiles, column tile after column tile within a group.
+    static __device__ __forceinline__ void tile(int t, int m_tiles, int n_tiles, int group, int &m, int &n) {
+        const int per = group * n_tiles;
+        const int g = t / per, first = g * group;
+        const int high = min(group, m_tiles - first), in = t - g * per;
+        m = first + in % high;
+        n = in / high;
+    }
+    template <int MODE>
+    __device__ __forceinline__ bool next(Unit &u) {
+        if (phase == 0) {
+            const int t = pair + i * pairs;
+            if (t < units) {
+                ++i;
+                const int split = t % splits;
+                u.dw = false;
+                tile(t / splits, m_tiles, n_tiles, group, u.m, u.n);
+                u.k0 = (int)((int64_t)k_blocks * split / splits);
+                u.k1 = (int)((int64_t)k_blocks * (split + 1) / splits);
+                u.place = ((int64_t)u.m * n_tiles + u.n) * splits + split;
+                return true;
+            }
+            phase = 1, i = 0;
+        }
+        if constexpr (MODE == kBack) {
+            int t = -1;
+            if (phase == 1) {
+                t = pair - rest + i * (pairs - rest);
+                if (pair < rest || i >= early_each || t >= early) phase = 2, i = 0;
+            }
+            if (phase == 2) t = early + pair + i * pairs;
+            if (t >= dw_units) return false;
+            ++i;
+            u.dw = true;
+            tile(t, dw_m, n_tiles, dw_group, u.m, u.n);
+            u.k0 = 0, u.k1 = dw_k;
+            return true;
+        }
+        return false;
+    }
+};
 
 template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
 template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
@@ -186,8 +250,7 @@ __device__ __forceinline__ float pick(int j, int at, float y, float z) {
 // of itself instead of 1.2e-6).
 template <int MODE, bool LONG, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1) __cluster_dims__(2, 1, 1)
-product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a2, const __grid_constant__ CUtensorMap map_b,
-               const __grid_constant__ CUtensorMap map_b2, const __grid_constant__ CUtensorMap map_out, const ProductArgs a) {
+product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ ProductArgs a) {
     extern __shared__ uint8_t raw[];
     __shared__ ProductShared s;
     uint8_t *tiles = (uint8_t *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
@@ -197,12 +260,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
     const int rows = a.head ? a.head->count : a.rows;
     const bool whole = a.head ? a.head->whole != 0 : true;
-    int m_tiles = a.m_tiles, k_blocks = a.k_blocks;
-    if (MODE == kDw) k_blocks = (rows + kK - 1) / kK;
-    else m_tiles = (rows + kM - 1) / kM;
-    const int total = m_tiles * a.n_tiles * a.splits;
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int pass = LONG ? kPass : k_blocks + 1;      // stages an accumulator takes
+    Work work;
+    work.begin<MODE>(a, rows);
+    const int k_blocks = a.k_blocks, pass = LONG ? kPass : INT32_MAX / 2;      // stages an accumulator takes
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
@@ -224,32 +284,35 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
     if (warp == 0 && lane == 0) {
         // ---- loads: this CTA's half of the rows of either operand
-        // the rows' operand: x, which is read where it is when every row takes part (A of the logits, B of dw)
-        const CUtensorMap *pa = MODE == kStats || MODE == kGrad ? (whole ? &map_a : &map_a2) : &map_a;
-        const CUtensorMap *pb = MODE == kDw ? (whole ? &map_b : &map_b2) : &map_b;
-        tma_prefetch_map(pa);
-        tma_prefetch_map(pb);
+        // (x is read where it is when every row takes part, else from the gathered copy)
         uint32_t it = 0;
         bool ok = true;
-        for (int t = pair; t < total && ok; t += pairs) {
-            const Tile tl = tile_at(t, m_tiles, a.n_tiles, a.group, a.splits);
-            const int k0 = (int)((int64_t)k_blocks * tl.split / a.splits), k1 = (int)((int64_t)k_blocks * (tl.split + 1) / a.splits);
-            const int m0 = tl.m * kM + rank * kHalf, n0 = tl.n * kN + rank * kHalf;
-            for (int k = k0; k < k1; ++k, ++it) {
+        Unit u;
+        while (ok && work.next<MODE>(u)) {
+            const CUtensorMap *pa, *pb;
+            if constexpr (MODE == kBack) {
+                pa = u.dw ? &maps.a2 : &maps.a;                                   // G, by either of its sides
+                pb = u.dw ? (whole ? &maps.b2 : &maps.b3) : &maps.b;              // x or w
+            } else {
+                pa = whole ? &maps.a : &maps.a2;                                  // x
+                pb = &maps.b;                                                     // w
+            }
+            const int m0 = u.m * kM + rank * kHalf, n0 = u.n * kN + rank * kHalf;
+            for (int k = u.k0; k < u.k1; ++k, ++it) {
                 const int st = it % kStages;
                 if (!(ok = wait_for(s, &s.empty[st], ((it / kStages) & 1) ^ 1))) break;
                 uint8_t *sa = tiles + st * kStage, *sb = sa + kOperand;
                 const uint32_t full = in_first(&s.full[st]);
                 if (rank == 0) mbar_arrive_expect_tx(&s.full[st], 2 * kStage);      // of both CTAs
-                if (MODE == kDw) {          // A: G, tokens by vocabulary; the vocabulary (rows of dw) is contiguous
+                if (MODE == kBack && u.dw) {          // A: G, tokens by vocabulary; the vocabulary (rows of dw) is contiguous
                     for (int h = 0; h < kHalf / 64; ++h) tma_load(sa + h * 8192, pa, m0 + h * 64, k * kK, full);
                 } else {
                     tma_load(sa, pa, k * kK, m0, full);
                 }
-                if (MODE == kStats || MODE == kGrad) {
+                if (MODE != kBack) {
                     tma_load(sb, pb, k * kK, (int)a.v0 + n0, full);
                 } else {                    // B: w or x, whose columns (of the result) are contiguous
-                    const int y = MODE == kDx ? (int)a.v0 + k * kK : k * kK;
+                    const int y = u.dw ? k * kK : (int)a.v0 + k * kK;
                     for (int h = 0; h < kHalf / 64; ++h) tma_load(sb + h * 8192, pb, n0 + h * 64, y, full);
                 }
             }
@@ -263,17 +326,20 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     } else if (warp == 1 && lane == 0 && rank == 0) {
         // ---- products
         constexpr uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
-        constexpr uint32_t a_rows_contiguous = MODE == kDw, b_rows_contiguous = MODE == kDx || MODE == kDw;
-        constexpr uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | (a_rows_contiguous << 15) | (b_rows_contiguous << 16) |
-                                   ((kN / 8) << 17) | ((kM / 16) << 24);
+        // operand rows: contiguous (1) or strided, by operand; bits 15 and 16 of the instruction's descriptor
+        constexpr uint32_t common = (1u << 4) | (type << 7) | (type << 10) | ((kN / 8) << 17) | ((kM / 16) << 24) | (MODE == kBack ? 1u << 16 : 0u);
         uint32_t it = 0, nth = 0;
         bool ok = true;
-        for (int t = pair; t < total && ok; t += pairs) {
-            const int split = t % a.splits;
-            const int k0 = (int)((int64_t)k_blocks * split / a.splits), k1 = (int)((int64_t)k_blocks * (split + 1) / a.splits);
+        Unit u;
+        while (ok && work.next<MODE>(u)) {
+            const int k0 = u.k0, k1 = u.k1;
+            const bool dw = MODE == kBack && u.dw;
+            const uint32_t idesc = common | (dw ? 1u << 15 : 0u);
+            // 16 deeper: 16 elements on in a row of 128 bytes, or, where the operand's rows are contiguous, 16 such rows on
+            const uint32_t a_step = dw ? 2048 : 32, b_step = MODE == kBack ? 2048 : 32;
             for (int p0 = k0; ok; p0 += pass, ++nth) {          // (once even where there is no depth)
                 const uint32_t acc = nth & 1;
-                const int p1 = min(k1, p0 + pass);
+                const int p1 = min(k1, LONG ? p0 + pass : k1);
                 if (!(ok = wait_for(s, &s.free_[acc], ((nth >> 1) & 1) ^ 1))) break;
                 tc_fence_after();
                 for (int k = p0; k < p1; ++k, ++it) {
@@ -283,9 +349,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     const uint8_t *sa = tiles + st * kStage, *sb = sa + kOperand;
 #pragma unroll
                     for (int j = 0; j < kK / 16; ++j) {
-                        // depth contiguous: 16 elements on in a row of 128 bytes; rows contiguous: 16 rows of 128 bytes on
-                        const uint64_t da = smem_desc(sa + (a_rows_contiguous ? j * 2048 : j * 32), 8192, 1024);
-                        const uint64_t db = smem_desc(sb + (b_rows_contiguous ? j * 2048 : j * 32), 8192, 1024);
+                        const uint64_t da = smem_desc(sa + j * a_step, 8192, 1024), db = smem_desc(sb + j * b_step, 8192, 1024);
                         tc_mma(tmem + acc * kN, da, db, idesc, k > p0 || j > 0);
                     }
                     tc_commit(&s.empty[st]);
@@ -311,12 +375,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         const float inverse = a.head ? a.head->inverse : 1.0f, unit = a.head ? a.head->unit : 1.0f, scale = a.head ? a.head->scale : 1.0f;
         const uint32_t free0 = in_first(&s.free_[0]), free1 = in_first(&s.free_[1]);
         uint32_t nth = 0;
-        for (int t = pair; t < total; t += pairs) {
-            const Tile tl = tile_at(t, m_tiles, a.n_tiles, a.group, a.splits);
-            const int row = tl.m * kM + rank * kHalf + quarter * 32 + lane;
-            bool empty = false;       // no depth at all: the accumulator was not written
-            if (MODE == kDw || MODE == kDx)
-                empty = (int)((int64_t)k_blocks * tl.split / a.splits) == (int)((int64_t)k_blocks * (tl.split + 1) / a.splits);
+        Unit u;
+        while (work.next<MODE>(u)) {
+            const int row = u.m * kM + rank * kHalf + quarter * 32 + lane;
+            const bool empty = u.k0 == u.k1;       // no depth at all: the accumulator was not written
             int64_t target = -1;
             float lse2 = 0.0f, g = 0.0f;
             if (MODE == kStats || MODE == kGrad) {
@@ -356,7 +418,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             ++nth;
             tc_fence_after();
             const uint32_t from = mine + acc * kN, freed = acc ? free1 : free0;
-            const int64_t col0 = (int64_t)tl.n * kN + half * 128;
+            const int64_t col0 = (int64_t)u.n * kN + half * 128;
             if constexpr (MODE == kStats) {
                 RowSum sums{-INFINITY, 0.0f};
                 constexpr int N = LONG ? 16 : 32;
@@ -394,11 +456,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     }
                     sums.add(z);
                 }
-                if (row < rows) a.parts[(int64_t)row * a.n_parts + tl.n * 2 + half] = make_float2(sums.top, sums.sum);
+                if (row < rows) a.parts[(int64_t)row * a.n_parts + u.n * 2 + half] = make_float2(sums.top, sums.sum);
             } else {
-                const bool partly = MODE == kDx && a.partial;
+                const bool dw = MODE == kBack && u.dw, dx = MODE == kBack && !u.dw, partly = dx && a.partial;
                 // (dx of gathered rows goes to the rows they come from; everything else is stored box by box)
-                const bool boxes = !partly && (MODE != kDx || whole);
+                const bool boxes = !partly && (!dx || whole);
+                const int64_t most = MODE == kGrad ? INT64_MAX : dx ? rows : a.vocab - a.v0;      // rows that are there
                 const int64_t left = MODE == kGrad ? a.vocab - a.v0 - col0 : a.width - col0;     // columns that are there
                 const int at = (int)max((int64_t)-1, min((int64_t)128, target - a.v0 - col0));
 #pragma unroll 1
@@ -428,10 +491,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                                 if (c * 32 + j >= left || row >= rows) x[j] = 0.0f;
                         }
                     } else if (partly) {
-                        const int64_t unit = ((int64_t)tl.m * a.n_tiles + tl.n) * a.splits + tl.split;
 #pragma unroll
                         for (int q = 0; q < 8; ++q) {
-                            float4 *p = a.partial + partial_at(unit, rank, half, quarter, c * 8 + q, lane);
+                            float4 *p = a.partial + partial_at(u.place, rank, half, quarter, c * 8 + q, lane);
                             float4 y = make_float4(__uint_as_float(r[4 * q]), __uint_as_float(r[4 * q + 1]), __uint_as_float(r[4 * q + 2]), __uint_as_float(r[4 * q + 3]));
                             if (empty) y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                             if (a.add) {
@@ -455,13 +517,13 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                             fence_to_tma();
                             __syncwarp();
                             // (row: of lane 0, the box's first; a box that starts outside the result is not stored)
-                            if (lane == 0 && (MODE == kGrad || ((c - 1) * 32 < left && row < (MODE == kDx ? rows : a.vocab - a.v0)))) {
-                                tma_store(&map_out, box, (int)(col0 + (c - 1) * 32), (int)(MODE == kDw ? a.v0 + row : row));
+                            if (lane == 0 && (MODE == kGrad || (c - 1) * 32 < left) && row < most) {
+                                tma_store(dw ? &maps.out2 : &maps.out, box, (int)(col0 + (c - 1) * 32), (int)(dw ? a.v0 + row : row));
                                 tma_store_commit();
                             }
                         }
                     } else if (row < rows) {
-                        store_row32(reinterpret_cast<T *>(a.out) + (int64_t)a.row_of[row] * a.out_stride + col0 + c * 32, (int)min((int64_t)32, left - c * 32), x);
+                        store_row32(reinterpret_cast<T *>(a.dx) + (int64_t)a.row_of[row] * a.dx_stride + col0 + c * 32, (int)min((int64_t)32, left - c * 32), x);
                     }
                 }
             }
@@ -499,16 +561,47 @@ __device__ __forceinline__ int64_t target_at(const void *t, int bits, int64_t i)
     return bits == 64 ? reinterpret_cast<const long long *>(t)[i] : (int64_t) reinterpret_cast<const int *>(t)[i];
 }
 
-// One CTA walks over the rows in order, eight a thread at a time.
-__global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a) {
-    constexpr int kEach = 8;
+struct GatherArgs {
+    const Header *head;
+    const int32_t *place;
+    int rows;
+    const void *x;
+    int64_t stride;
+    int vectors;           // 16-byte vectors of a row
+    void *to;              // [padded][vectors]
+    void *dx;              // or NULL: rows that take no part become zero
+};
+
+// A warp copies a row that takes part to its place, or clears its gradient.
+__device__ __forceinline__ void gather_row(const GatherArgs &a, int64_t r, int at) {
+    const uint4 *from = reinterpret_cast<const uint4 *>((const char *)a.x + r * a.stride * 2);
+    uint4 *to = at >= 0 ? reinterpret_cast<uint4 *>(a.to) + (int64_t)at * a.vectors : a.dx ? reinterpret_cast<uint4 *>(a.dx) + r * a.vectors : nullptr;
+    if (!to) return;
+    for (int v = lane_id(); v < a.vectors; v += 32) to[v] = at >= 0 ? from[v] : make_uint4(0, 0, 0, 0);
+}
+// Rows of the gathered copy behind the last one, up to a whole tile: zeros.
+__device__ __forceinline__ void pad_rows(const GatherArgs &a, int count, int warp, int warps) {
+    const int padded = (count + kM - 1) / kM * kM;
+    for (int64_t p = count + warp; p < padded; p += warps)
+        for (int v = lane_id(); v < a.vectors; v += 32) reinterpret_cast<uint4 *>(a.to)[p * a.vectors + v] = make_uint4(0, 0, 0, 0);
+}
+
+// Finds the rows that take part: a CTA walks over all rows in order, eight a thread at a time.  GATHER (up to kWalk rows):
+// every CTA of the grid does so for itself and gathers a slice of the rows, which saves a launch; the first one writes what
+// the products read.
+constexpr int kEach = 8, kWalk = 1024 * kEach, kSlice = 256;
+template <bool GATHER>
+__global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a, const GatherArgs ga, int slice) {
     __shared__ int s_count[32];
     __shared__ float s_top[32];
+    __shared__ int s_place[kSlice];
     pdl_wait();
     const int lane = lane_id(), warp = warp_id();
+    const bool writes = blockIdx.x == 0;
+    const int64_t slice0 = (int64_t)blockIdx.x * slice;
     int before = 0;
     float top = 0.0f;
-    for (int64_t base = 0; base < a.rows; base += 1024 * kEach) {
+    for (int64_t base = 0; base < a.rows; base += kWalk) {
         const int64_t first = base + threadIdx.x * kEach;
         int64_t t[kEach];
         float g[kEach];
@@ -516,7 +609,7 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a) {
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             t[j] = first + j < a.rows ? target_at(a.targets, a.bits, first + j) : a.ignore;
-            g[j] = a.grads && first + j < a.rows ? a.grad[(first + j) * a.grad_stride] : 0.0f;
+            g[j] = writes && a.grads && first + j < a.rows ? a.grad[(first + j) * a.grad_stride] : 0.0f;
         }
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
@@ -524,7 +617,7 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a) {
             if (t[j] != a.ignore && !bad) {
                 in |= 1u << j;
                 top = fmaxf(top, fabsf(g[j]));
-            } else if (first + j < a.rows) {
+            } else if (writes && first + j < a.rows) {
                 if (bad && a.status) atomicOr(a.status, kStatIndex);
                 if (a.loss) {
                     a.loss[first + j] = bad ? __uint_as_float(0x7FC00000u) : 0.0f;
@@ -547,7 +640,7 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a) {
         for (int j = 0; j < kEach; ++j) {
             if (first + j >= a.rows) continue;
             const bool takes = (in >> j) & 1;
-            if (takes) {
+            if (takes && writes) {
                 a.target[at] = (int32_t)t[j];
                 a.row_of[at] = (int32_t)(first + j);
                 if (a.grads) {
@@ -555,12 +648,21 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a) {
                     a.grad_to[at] = g[j];
                 }
             }
-            a.place[first + j] = takes ? at : -1;
+            if (GATHER) {
+                if (first + j >= slice0 && first + j < slice0 + slice) s_place[first + j - slice0] = takes ? at : -1;
+            } else {
+                a.place[first + j] = takes ? at : -1;
+            }
             at += takes;
         }
         before += all;
         __syncthreads();
     }
+    if (GATHER && before != a.rows) {
+        for (int64_t r = warp; r < slice && slice0 + r < a.rows; r += 32) gather_row(ga, slice0 + r, s_place[r]);
+        pad_rows(ga, before, blockIdx.x * 32 + warp, gridDim.x * 32);
+    }
+    if (!writes) return;
     for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
     if (lane == 0) s_top[warp] = top;
     __syncthreads();
@@ -575,39 +677,13 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a) {
     }
 }
 
-struct GatherArgs {
-    const Header *head;
-    const int32_t *place;
-    int rows, padded;
-    const void *x;
-    int64_t stride;
-    int vectors;           // 16-byte vectors of a row
-    void *to;              // [padded][vectors]
-    void *dx;              // or NULL: rows that take no part become zero
-};
-
-// Gathers the rows that take part, with zeros up to a whole tile; a warp per row.
+// Gathers the rows that take part, where the walk has not done so; a warp per row.
 __global__ void __launch_bounds__(256) xent_gather_kernel(const GatherArgs a) {
     pdl_wait();
     if (a.head->whole) return;
-    const int count = a.head->count;
-    const int padded = (count + kM - 1) / kM * kM;
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    for (int64_t r = (int64_t)blockIdx.x * 8 + warp_id(); r < a.rows + kM; r += (int64_t)gridDim.x * 8) {
-        if (r >= a.rows) {             // padding rows
-            const int64_t p = count + (r - a.rows);
-            if (p < padded)
-                for (int v = lane_id(); v < a.vectors; v += 32) reinterpret_cast<uint4 *>(a.to)[p * a.vectors + v] = zero;
-            continue;
-        }
-        const int at = a.place[r];
-        if (at >= 0) {
-            const uint4 *from = reinterpret_cast<const uint4 *>((const char *)a.x + r * a.stride * 2);
-            for (int v = lane_id(); v < a.vectors; v += 32) reinterpret_cast<uint4 *>(a.to)[(int64_t)at * a.vectors + v] = from[v];
-        } else if (a.dx) {
-            for (int v = lane_id(); v < a.vectors; v += 32) reinterpret_cast<uint4 *>(a.dx)[r * a.vectors + v] = zero;
-        }
-    }
+    const int warp = blockIdx.x * 8 + warp_id(), warps = gridDim.x * 8;
+    for (int64_t r = warp; r < a.rows; r += warps) gather_row(a, r, a.place[r]);
+    pad_rows(a, a.head->count, warp, warps);
 }
 
 struct CombineArgs {
@@ -674,7 +750,7 @@ struct JoinArgs {
     const int32_t *row_of;
     int64_t width;
     const float4 *partial;
-    int n_tiles, splits;
+    int n_tiles, max_units, max_splits;
     void *dx;
 };
 
@@ -683,7 +759,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) xent_join_kernel(const JoinArgs a) {
     pdl_wait();
     const int rows = a.head->count;
-    const int64_t m_tiles = (rows + kM - 1) / kM, work = m_tiles * a.n_tiles * 256;       // (16 warps of a tile, 16 pairs of groups)
+    const int tiles = (rows + kM - 1) / kM * a.n_tiles, splits = dx_splits(tiles, a.max_units, a.max_splits);
+    const int64_t work = (int64_t)tiles * 256;       // (16 warps of a tile, 16 pairs of groups)
     const float inverse = a.head->inverse;
     const bool whole = a.head->whole != 0;
     for (int64_t i = (int64_t)blockIdx.x * 8 + warp_id(); i < work; i += (int64_t)gridDim.x * 8) {
@@ -694,8 +771,8 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const JoinArgs a) {
         const int64_t col = tile % a.n_tiles * kN + half * 128 + pair * 8;
         if (col >= a.width) continue;
         float x[8] = {};
-        for (int k = 0; k < a.splits; ++k) {
-            const float4 *p = a.partial + partial_at(tile * a.splits + k, rank, half, quarter, pair * 2, lane_id());
+        for (int k = 0; k < splits; ++k) {
+            const float4 *p = a.partial + partial_at(tile * splits + k, rank, half, quarter, pair * 2, lane_id());
             const float4 u = p[0], v = p[32];
             const float y[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -711,6 +788,21 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const JoinArgs a) {
 // ---- host ------------------------------------------------------------------------------------------------------------
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+// Allows a kernel its shared memory, once per device.
+struct SmemAttribute {
+    std::atomic<uint64_t> done{0};
+    cudaError_t set(const void *kernel, int bytes) {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+        if (bit & done.load(std::memory_order_relaxed)) return cudaSuccess;
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+        return e;
+    }
+};
 
 PFN_cuTensorMapEncodeTiled encoder() {
     static PFN_cuTensorMapEncodeTiled fn = [] {
@@ -742,7 +834,7 @@ constexpr int kDirectRows = kHalf;     // up to here the forward pass takes the 
 struct XentLayout {
     size_t head, target, row_of, place, lse, grad, picked, parts, x, g, partial, total;
     int64_t padded, piece;
-    int n_parts, splits;
+    int n_parts, max_units, max_splits;     // max_units 0: dx is written directly
 };
 
 // What a row tile's share of the second-level cache allows the G of one piece to take.
@@ -773,30 +865,29 @@ XentLayout layout(int64_t rows, int64_t width, int64_t vocab, bool grads) {
         L.piece = piece;
         take(L.g, (size_t)L.padded * piece * 2);
         const int64_t tiles = L.padded / kM * ((width + kN - 1) / kN);
-        int64_t splits = sm_count() / 2 / tiles;
-        const int64_t depth = piece / kK;
-        if (splits > depth / 4) splits = depth / 4;
-        if (splits < 1) splits = 1;
-        L.splits = (int)splits;
-        take(L.partial, splits > 1 || pieces > 1 ? (size_t)(splits * tiles * kPartialTile) * sizeof(float4) : 0);
+        const int64_t pairs = sm_count() / 2;
+        L.max_splits = (int)(piece / kK / 4 > 1 ? piece / kK / 4 : 1);
+        const bool split = tiles * 2 <= pairs && L.max_splits > 1;
+        L.max_units = (int)(!split && pieces == 1 ? 0 : tiles > pairs ? tiles : pairs);
+        take(L.partial, (size_t)(L.max_units * kPartialTile) * sizeof(float4));
     }
     L.total = off;
     return L;
 }
 
 template <int MODE, bool LONG, typename T>
-cudaError_t launch_product_as(const CUtensorMap &ma, const CUtensorMap &ma2, const CUtensorMap &mb, const CUtensorMap &mb2, const CUtensorMap &mo, const ProductArgs &a, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(product_kernel<MODE, LONG, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
+cudaError_t launch_product_as(const Maps &maps, const ProductArgs &a, int64_t units, cudaStream_t st) {
+    static SmemAttribute wide;
+    const cudaError_t e = wide.set((const void *)product_kernel<MODE, LONG, T>, kProductSmem);
     if (e != cudaSuccess) return e;
-    const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * a.splits;
     const int64_t pairs = sm_count() / 2;
-    return launch_after_smem(product_kernel<MODE, LONG, T>, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), dim3(kProductThreads), kProductSmem, st, ma, ma2, mb, mb2, mo, a);
+    return launch_after_smem(product_kernel<MODE, LONG, T>, dim3((unsigned)(2 * (units < pairs ? units : pairs))), dim3(kProductThreads), kProductSmem, st, maps, a);
 }
 template <int MODE, typename T>
-cudaError_t launch_product(const CUtensorMap &ma, const CUtensorMap &ma2, const CUtensorMap &mb, const CUtensorMap &mb2, const CUtensorMap &mo, const ProductArgs &a, cudaStream_t st) {
+cudaError_t launch_product(const Maps &maps, const ProductArgs &a, int64_t units, cudaStream_t st) {
     if constexpr (MODE == kStats)
-        if (a.k_blocks > kPass) return launch_product_as<MODE, true, T>(ma, ma2, mb, mb2, mo, a, st);
-    return launch_product_as<MODE, false, T>(ma, ma2, mb, mb2, mo, a, st);
+        if (a.k_blocks > kPass) return launch_product_as<MODE, true, T>(maps, a, units, st);
+    return launch_product_as<MODE, false, T>(maps, a, units, st);
 }
 
 // Row tiles that share a column tile: as many as fit in about a third of the second-level cache.
@@ -832,20 +923,26 @@ cudaError_t launch_rows(const XentArgs &x, const XentLayout &L, bool grads, cuda
         r.loss = x.loss;
         r.lse_out = x.lse_out;
     }
-    cudaError_t e = launch_after(xent_rows_kernel, dim3(1), dim3(1024), st, r);
-    if (e != cudaSuccess) return e;
     GatherArgs g{};
     g.head = r.head;
     g.place = r.place;
     g.rows = r.rows;
-    g.padded = r.padded;
     g.x = x.x;
     g.stride = x.x_stride;
     g.vectors = (int)(x.width / 8);
     g.to = ws + L.x;
     g.dx = grads ? x.dx : nullptr;
-    int64_t grid = (x.rows + kM + 7) / 8;
-    if (grid > sm_count() * 8) grid = sm_count() * 8;
+    const int64_t sms = sm_count();
+    if (x.rows <= kWalk) {
+        int64_t grid = (x.rows + 7) / 8;
+        if (grid > sms) grid = sms;
+        const int64_t slice = (x.rows + grid - 1) / grid;
+        if (slice <= kSlice) return launch_after(xent_rows_kernel<true>, dim3((unsigned)grid), dim3(1024), st, r, g, (int)slice);
+    }
+    const cudaError_t e = launch_after(xent_rows_kernel<false>, dim3(1), dim3(1024), st, r, g, 0);
+    if (e != cudaSuccess) return e;
+    int64_t grid = (x.rows + 7) / 8;
+    if (grid > sms * 8) grid = sms * 8;
     return launch_after(xent_gather_kernel, dim3((unsigned)grid), dim3(256), st, g);
 }
 
@@ -855,11 +952,11 @@ cudaError_t forward(const XentArgs &x, cudaStream_t st) {
     char *ws = (char *)x.workspace;
     const bool direct = x.rows <= kDirectRows, bf16 = x.dtype == 1;
     cudaError_t e;
-    CUtensorMap mx, mg, mw;
-    if (!make_map(&mx, bf16, x.x, x.width, x.rows, x.x_stride, kHalf) || !make_map(&mw, bf16, x.w, x.width, x.vocab, x.w_stride, kHalf)) return cudaErrorInvalidValue;
-    mg = mx;
+    Maps maps{};
+    if (!make_map(&maps.a, bf16, x.x, x.width, x.rows, x.x_stride, kHalf) || !make_map(&maps.b, bf16, x.w, x.width, x.vocab, x.w_stride, kHalf)) return cudaErrorInvalidValue;
+    maps.a2 = maps.a;
     if (!direct) {
-        if (!make_map(&mg, bf16, ws + L.x, x.width, L.padded, x.width, kHalf)) return cudaErrorInvalidValue;
+        if (!make_map(&maps.a2, bf16, ws + L.x, x.width, L.padded, x.width, kHalf)) return cudaErrorInvalidValue;
         e = launch_rows(x, L, false, st);
         if (e != cudaSuccess) return e;
     }
@@ -871,7 +968,6 @@ cudaError_t forward(const XentArgs &x, cudaStream_t st) {
     a.m_tiles = (int)(L.padded / kM);
     a.n_tiles = (int)((x.vocab + kN - 1) / kN);
     a.k_blocks = (int)((x.width + kK - 1) / kK);
-    a.splits = 1;
     a.group = group_of(x.width * 2, a.m_tiles);
     a.target = direct ? nullptr : (const int32_t *)(ws + L.target);
     a.raw_target = x.targets;
@@ -880,7 +976,7 @@ cudaError_t forward(const XentArgs &x, cudaStream_t st) {
     a.n_parts = L.n_parts;
     a.picked = (float *)(ws + L.picked);
     a.status = x.status;
-    e = launch_product<kStats, T>(mx, mg, mw, mw, mw, a, st);
+    e = launch_product<kStats, T>(maps, a, (int64_t)a.m_tiles * a.n_tiles, st);
     if (e != cudaSuccess) return e;
     CombineArgs c{};
     c.head = a.head;
@@ -908,17 +1004,17 @@ cudaError_t backward(const XentArgs &x, cudaStream_t st) {
     const bool bf16 = x.dtype == 1;
     cudaError_t e = launch_rows(x, L, true, st);
     if (e != cudaSuccess) return e;
-    CUtensorMap mx, mxg, mw, gk, gm, wn, xn, xng, go, xo, wo;
-    // G as the rows' operand of dx (its vocabulary is the depth) and of dw (its vocabulary are the rows)
-    if (!make_map(&mx, bf16, x.x, x.width, x.rows, x.x_stride, kHalf) || !make_map(&mxg, bf16, ws + L.x, x.width, L.padded, x.width, kHalf) ||
-        !make_map(&mw, bf16, x.w, x.width, x.vocab, x.w_stride, kHalf) || !make_map(&gk, bf16, ws + L.g, L.piece, L.padded, L.piece, kHalf) ||
-        !make_map(&gm, bf16, ws + L.g, L.piece, L.padded, L.piece, kK) || !make_map(&wn, bf16, x.w, x.width, x.vocab, x.w_stride, kK) ||
-        !make_map(&xn, bf16, x.x, x.width, x.rows, x.x_stride, kK) || !make_map(&xng, bf16, ws + L.x, x.width, L.padded, x.width, kK) ||
-        !make_map(&go, bf16, ws + L.g, L.piece, L.padded, L.piece, 32) || (x.dx && !make_map(&xo, bf16, x.dx, x.width, x.rows, x.width, 32)) ||
-        (x.dw && !make_map(&wo, bf16, x.dw, x.width, x.vocab, x.width, 32)))
+    Maps logits{}, back{};
+    // logits: x, gathered x, w, G.  back: G by its rows (the depth of dx is the vocabulary) and by its columns (the rows of
+    // dw), w and x with the result's columns contiguous, dx, dw
+    if (!make_map(&logits.a, bf16, x.x, x.width, x.rows, x.x_stride, kHalf) || !make_map(&logits.a2, bf16, ws + L.x, x.width, L.padded, x.width, kHalf) ||
+        !make_map(&logits.b, bf16, x.w, x.width, x.vocab, x.w_stride, kHalf) || !make_map(&logits.out, bf16, ws + L.g, L.piece, L.padded, L.piece, 32) ||
+        !make_map(&back.a, bf16, ws + L.g, L.piece, L.padded, L.piece, kHalf) || !make_map(&back.a2, bf16, ws + L.g, L.piece, L.padded, L.piece, kK) ||
+        !make_map(&back.b, bf16, x.w, x.width, x.vocab, x.w_stride, kK) || !make_map(&back.b2, bf16, x.x, x.width, x.rows, x.x_stride, kK) ||
+        !make_map(&back.b3, bf16, ws + L.x, x.width, L.padded, x.width, kK) || (x.dx && !make_map(&back.out, bf16, x.dx, x.width, x.rows, x.width, 32)) ||
+        (x.dw && !make_map(&back.out2, bf16, x.dw, x.width, x.vocab, x.width, 32)))
         return cudaErrorInvalidValue;
     const int64_t pieces = (x.vocab + L.piece - 1) / L.piece;
-    const bool direct = L.splits == 1 && pieces == 1;
     ProductArgs a{};
     a.head = (const Header *)(ws + L.head);
     a.rows = (int)x.rows;
@@ -937,42 +1033,36 @@ cudaError_t backward(const XentArgs &x, cudaStream_t st) {
         g.m_tiles = row_tiles;
         g.n_tiles = (int)((here + kN - 1) / kN);
         g.k_blocks = (int)((x.width + kK - 1) / kK);
-        g.splits = 1;
         g.group = group_of(x.width * 2, g.m_tiles);
-        e = launch_product<kGrad, T>(mx, mxg, mw, mw, go, g, st);
+        e = launch_product<kGrad, T>(logits, g, (int64_t)g.m_tiles * g.n_tiles, st);
         if (e != cudaSuccess) return e;
-        if (x.dx) {
-            ProductArgs d = a;
-            d.m_tiles = row_tiles;
-            d.n_tiles = width_tiles;
-            d.k_blocks = (int)((here + kK - 1) / kK);
-            d.splits = L.splits;
-            d.group = row_tiles < 8 ? row_tiles : 8;
-            d.out = x.dx;
-            d.out_stride = x.width;
-            d.partial = direct ? nullptr : (float4 *)(ws + L.partial);
-            d.add = p > 0;
-            e = launch_product<kDx, T>(gk, gk, wn, wn, xo, d, st);
-            if (e != cudaSuccess) return e;
-        }
-        if (x.dw) {
-            ProductArgs d = a;
-            d.m_tiles = (int)((here + kM - 1) / kM);
-            d.n_tiles = width_tiles;
-            d.splits = 1;
-            d.group = d.m_tiles < 8 ? d.m_tiles : 8;
-            e = launch_product<kDw, T>(gm, gm, xn, xng, wo, d, st);
-            if (e != cudaSuccess) return e;
-        }
+        ProductArgs d = a;
+        d.n_tiles = width_tiles;
+        d.k_blocks = (int)((here + kK - 1) / kK);
+        d.m_tiles = x.dx ? row_tiles : 0;
+        d.group = row_tiles < 8 ? row_tiles : 8;
+        d.dw_tiles = x.dw ? (int)((here + kM - 1) / kM) : 0;
+        d.dw_group = d.dw_tiles < 8 ? d.dw_tiles : 8;
+        d.dx = x.dx;
+        d.dx_stride = x.width;
+        d.partial = L.max_units ? (float4 *)(ws + L.partial) : nullptr;
+        d.max_units = L.max_units;
+        d.max_splits = L.max_splits;
+        d.add = p > 0;
+        // (one launch for both: tiles of dw fill the pairs that a last round of dx leaves idle)
+        const int64_t dx_units = !x.dx ? 0 : L.max_units ? L.max_units : (int64_t)row_tiles * width_tiles;
+        e = launch_product<kBack, T>(back, d, dx_units + (int64_t)d.dw_tiles * width_tiles, st);
+        if (e != cudaSuccess) return e;
     }
-    if (x.dx && !direct) {
+    if (x.dx && L.max_units) {
         JoinArgs j{};
         j.head = a.head;
         j.row_of = a.row_of;
         j.width = x.width;
         j.partial = (const float4 *)(ws + L.partial);
         j.n_tiles = width_tiles;
-        j.splits = L.splits;
+        j.max_units = L.max_units;
+        j.max_splits = L.max_splits;
         j.dx = x.dx;
         int64_t grid = (int64_t)row_tiles * width_tiles * 32;
         if (grid > sm_count() * 8) grid = sm_count() * 8;
