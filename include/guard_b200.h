@@ -418,7 +418,7 @@ int guard_embed_grad(const void *d_grad, int64_t stride, int dtype, const void *
  * Softmax cross entropy of a vocabulary product, without keeping the logits: with z = x w^T in float32,
  *   lse[n] = log sum over v of exp(z[n][v]);  loss[n] = lse[n] - z[n][target[n]].
  * d_x: [rows][width], d_w: [vocab][width], of type dtype (GUARD_BF16 or GUARD_F16), 16-byte aligned, strides
- * multiples of 8 elements, width a multiple of 8.  d_targets: [rows] int32 or int64 (target_bits).  Rows whose
+ * multiples of 8 elements, width a multiple of 8; rows <= 2^26.  d_targets: [rows] int32 or int64 (target_bits).  Rows whose
  * target is ignore_index are left out: loss and lse are 0, and what they hold reaches nothing.  A target
  * that is neither ignore_index nor in 0..vocab-1 sets GUARD_STATUS_INDEX, gives a loss of NaN and an lse of 0,
  * and is left out of the gradients.  Logits that are not finite give losses and gradients that are not.
@@ -457,7 +457,8 @@ int guard_linear_xent_grad(const void *d_x, int64_t x_stride, const void *d_w, i
  *
  * guard_adamw_create copies the table of tensors into the workspace (on `stream`, from host memory; the
  * addresses must stay valid until guard_adamw_destroy; parameters must not overlap one another).
- * `step`: updates made so far (0 for new states).  guard_adamw_step makes one update of all tensors and
+ * eps >= 1e-30 (second moments below 2^-126 count as zero beside it).  `step`: updates made so far (0 for
+ * new states).  guard_adamw_step makes one update of all tensors and
  * counts it on the device, so that a captured step counts each replay; lr is taken from d_lr (device, one
  * float32) where that is not NULL, so that a replay can use another one; d_grad_scale: device, one float32,
  * or NULL for 1.  guard_adamw_steps reads the counter back (synchronises).  Updates of one object must be

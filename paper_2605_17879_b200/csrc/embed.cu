@@ -157,7 +157,8 @@ struct SortArgs {
     EmbedGradArgs a;
     const uint32_t *in_key, *in_pos;   // the previous digit's order (unused for the first digit)
     uint32_t *out_key, *out_pos;
-    uint32_t *counts;                  // [tiles][kDigits]
+    uint32_t *counts;                  // [tiles][kDigits], then [kDigits] totals
+    bool scanned;                      // counts hold the numbers before each tile, totals theirs
     int64_t tiles;
     int shift, digits, first;
 };
@@ -194,6 +195,28 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_count_kernel(const So
     s.counts[(int64_t)blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
 }
 
+// Many tiles: turns the counts into the numbers before each tile, 32 digits a CTA, a part of the tiles a warp.
+__global__ void __launch_bounds__(1024) embed_sort_scan_kernel(uint32_t *counts, int64_t tiles) {
+    __shared__ uint32_t part[32][32];
+    pdl_wait();
+    const int lane = lane_id(), warp = warp_id();
+    const int64_t each = (tiles + 31) / 32, begin = min(tiles, warp * each), end = min(tiles, begin + each);
+    uint32_t *c = counts + blockIdx.x * 32 + lane;
+    uint32_t sum = 0;
+#pragma unroll 8
+    for (int64_t t = begin; t < end; ++t) sum += c[t * kDigits];
+    part[warp][lane] = sum;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int w = 0; w < warp; ++w) before += part[w][lane];
+    for (int64_t t = begin; t < end; ++t) {
+        const uint32_t x = c[t * kDigits];
+        c[t * kDigits] = before;
+        before += x;
+    }
+    if (warp == 31) c[tiles * kDigits] = before;
+}
+
 // Moves a tile's keys to their places in the digit's order.
 __global__ void __launch_bounds__(kSortThreads) embed_sort_move_kernel(const SortArgs s) {
     __shared__ SortShared sh;
@@ -202,11 +225,16 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_move_kernel(const Sor
     bool have[kSortItems];
     load_tile(s, blockIdx.x, key, pos, have);
     uint32_t all = 0, mine = 0;
+    if (s.scanned) {
+        mine = s.counts[(int64_t)blockIdx.x * kDigits + threadIdx.x];
+        all = s.counts[s.tiles * kDigits + threadIdx.x];
+    } else {
 #pragma unroll 8
-    for (int64_t t = 0; t < s.tiles; ++t) {
-        const uint32_t c = s.counts[t * kDigits + threadIdx.x];
-        if (t < blockIdx.x) mine += c;
-        all += c;
+        for (int64_t t = 0; t < s.tiles; ++t) {
+            const uint32_t c = s.counts[t * kDigits + threadIdx.x];
+            if (t < blockIdx.x) mine += c;
+            all += c;
+        }
     }
     rank_tile(sh, key, have, s.shift, rank);
     warps_before(sh);
@@ -590,7 +618,7 @@ GradLayout grad_layout(int64_t n, int64_t rows, int64_t width) {
         L.key[i] = off, off = up256(off + (size_t)n * 4);
         L.pos[i] = off, off = up256(off + (size_t)n * 4);
     }
-    L.counts = off, off = up256(off + (size_t)L.tiles * kDigits * 4);
+    L.counts = off, off = up256(off + (size_t)(L.tiles + 1) * kDigits * 4);
     // two lists of partial sums, used in turn
     int64_t m = next_length(n);
     for (int i = 0; i < 2; ++i) {
@@ -688,6 +716,10 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
             s.out_key = (uint32_t *)(ws + L.key[at]);
             s.out_pos = (uint32_t *)(ws + L.pos[at]);
             e = launch_after(embed_sort_count_kernel, dim3((unsigned)L.tiles), dim3(kSortThreads), st, s);
+            if (e != cudaSuccess) return e;
+            // (each CTA of the move adds the counts of all tiles up itself where they are few)
+            s.scanned = L.tiles > 64;
+            if (s.scanned) e = launch_after(embed_sort_scan_kernel, dim3(kDigits / 32), dim3(1024), st, s.counts, L.tiles);
             if (e != cudaSuccess) return e;
             e = launch_after(embed_sort_move_kernel, dim3((unsigned)L.tiles), dim3(kSortThreads), st, s);
             if (e != cudaSuccess) return e;

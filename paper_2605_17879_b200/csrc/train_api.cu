@@ -137,7 +137,7 @@ int guard_embed_grad(const void *d_grad, int64_t stride, int dtype, const void *
 }
 
 size_t guard_linear_xent_workspace_bytes(int64_t rows, int64_t width, int64_t vocab, int grads) {
-    if (rows < 1 || rows > (1LL << 30) || width < 8 || width > (1 << 24) || width % 8 || vocab < 1 || vocab > (1LL << 30)) return 0;
+    if (rows < 1 || rows > (1LL << 26) || width < 8 || width > (1 << 24) || width % 8 || vocab < 1 || vocab > (1LL << 30)) return 0;
     // tiles are counted in 32 bits (at most 148 splits of the depth)
     if (((rows + 127) / 128) * ((vocab + 255) / 256) > (1LL << 30) || ((rows + 127) / 128) * ((width + 255) / 256) > (1LL << 23) ||
         ((vocab + 127) / 128) * ((width + 255) / 256) > (1LL << 30))
@@ -150,7 +150,7 @@ static int xent_check(const XentArgs &a, size_t need, size_t given, const void *
     if ((a.dtype != GUARD_BF16 && a.dtype != GUARD_F16) || (a.target_bits != 32 && a.target_bits != 64))
         return call_error(GUARD_ERR_ARG, "dtype must be GUARD_BF16 or GUARD_F16, target_bits 32 or 64");
     if (need == 0 || a.x_stride < a.width || a.w_stride < a.width || a.x_stride % 8 || a.w_stride % 8 || a.x_stride >= (1LL << 36) || a.w_stride >= (1LL << 36))
-        return call_error(GUARD_ERR_ARG, "invalid sizes: need 1 <= vocab <= 2^30, rows <= 2^30, width a multiple of 8 up to 2^24, strides multiples of 8 and >= width, and a product that tiles");
+        return call_error(GUARD_ERR_ARG, "invalid sizes: need 1 <= vocab <= 2^30, rows <= 2^26, width a multiple of 8 up to 2^24, strides multiples of 8 and >= width, and a product that tiles");
     if (!a.x || !a.w || !a.targets) return call_error(GUARD_ERR_ARG, "d_x, d_w or d_targets is NULL");
     if (!on(a.x, 16) || !on(a.w, 16) || !on(a.targets, a.target_bits / 8)) return call_error(GUARD_ERR_ARG, "d_x and d_w must be 16-byte aligned, d_targets to its elements");
     if (!a.workspace || !on(a.workspace, 256) || given < need)
@@ -257,8 +257,8 @@ int guard_adamw_create(guard_adamw **out, const guard_adamw_tensor *tensors, int
     if (n < 1 || need == 0) return call_error(GUARD_ERR_ARG, "need at least one tensor, counts >= 0");
     if (!good_dtype(grad_dtype) || !good_dtype(copy_dtype)) return call_error(GUARD_ERR_ARG, "grad_dtype and copy_dtype must be GUARD_F32, _BF16 or _F16");
     if (state_bits != 8 && state_bits != 32) return call_error(GUARD_ERR_ARG, "state_bits must be 8 or 32");
-    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !std::isfinite(eps) || step < 0)
-        return call_error(GUARD_ERR_ARG, "need 0 <= beta < 1, a finite eps >= 0 and step >= 0");
+    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 1e-30) || !std::isfinite((float)eps) || step < 0)
+        return call_error(GUARD_ERR_ARG, "need 0 <= beta < 1, 1e-30 <= eps finite in float32, and step >= 0");
     const int64_t blocks = guard_adamw_blocks(tensors, n);
     if (blocks > 0 && (!d_m || !d_v || !on(d_m, 32) || !on(d_v, 32))) return call_error(GUARD_ERR_ARG, "d_m and d_v must be non-NULL and 32-byte aligned");
     if (blocks > 0 && state_bits == 8 && (!d_m_scale || !d_v_scale || !on(d_m_scale, 4) || !on(d_v_scale, 4)))

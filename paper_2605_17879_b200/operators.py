@@ -7,7 +7,7 @@ recorded for autograd: a gradient is a call of its own.
 
 Errors in data (a token outside its table) cannot be raised by the call that meets them without waiting for the GPU: they
 are kept in a status word per device, which sync_status() reads and clears, or in the uint32 tensor that the caller passes
-as out["status"].
+as out["status"].  The first call on a device makes that word and waits for it: make it before capturing a graph.
 """
 from __future__ import annotations
 

@@ -89,7 +89,8 @@ def check_grad(got, want, size, count, dtype):
 @pytest.mark.parametrize("n,rows,width,pad,kind", [
     (1, 1, 1, 0, "uniform"), (1, 70000, 8, 0, "uniform"), (64, 3, 16, 0, "uniform"), (65, 2, 1001, 0, "one"), (129, 513, 100, 4, "uniform"),
     (2048, 511, 64, 0, "zipf"), (2049, 512, 24, 0, "zipf"), (5003, 32001, 72, 1, "zipf"), (4096, 300000, 8, 0, "uniform"),
-    (1500, 10, 2056, 0, "one"), (9000, 5, 40, 0, "one"), (6000, 262144, 16, 0, "ends"), (40000, 1000, 33, 0, "zipf")])
+    (1500, 10, 2056, 0, "one"), (9000, 5, 40, 0, "one"), (6000, 262144, 16, 0, "ends"), (40000, 1000, 33, 0, "zipf"), (8192, 600, 8, 0, "zipf"), (8193, 600, 8, 0, "zipf"), (131073, 700, 8, 0, "zipf"),
+    (300001, 1000000, 8, 0, "uniform")])
 def test_embed_grad(ops, dtype, n, rows, width, pad, kind):
     g = gen(n + rows)
     grad = randn(g, n, width + pad).to(dtype)[:, :width]

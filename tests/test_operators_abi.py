@@ -51,7 +51,7 @@ def test_embed_grad_refusals(L):
 def test_cross_entropy_refusals(L):
     need = {g: L.guard_linear_xent_workspace_bytes(300, 64, 1000, g) for g in (0, 1)}
     assert need[0] > 0 and need[1] > need[0] and need[0] % 256 == 0 and need[1] % 256 == 0
-    for bad in ((0, 64, 1000), (300, 0, 1000), (300, 60, 1000), (300, 64, 0), (1 << 31, 64, 1000), (300, 64, 1 << 31), (1 << 30, 64, 1 << 30), (300, 1 << 25, 1000)):
+    for bad in ((0, 64, 1000), (300, 0, 1000), (300, 60, 1000), (300, 64, 0), ((1 << 26) + 1, 64, 1000), (300, 64, 1 << 31), (1 << 30, 64, 1 << 30), (300, 1 << 25, 1000)):
         assert L.guard_linear_xent_workspace_bytes(*bad, 0) == 0, bad
     big = 1 << 40
     def forward(x=P, xs=64, w=Q, wst=64, n=300, d=64, v=1000, dtype=1, t=WS, bits=64, loss=WS + big, lse=WS + big + 4096, ws=WS + 2 * big, nws=need[0]):
@@ -81,7 +81,7 @@ def test_adamw_refusals(L):
         t = (ops._AdamwTensor * max(1, len(tensors)))(*[ops._AdamwTensor(*x) for x in tensors])
         return L.guard_adamw_create(C.byref(h), t, len(tensors) if n is None else n, gt, ct, bits, b1, b2, eps, m, v, ms, vs, step, 0, ws, nws, None)
     inf = float("inf")
-    for bad in (dict(n=0), dict(n=-1), dict(gt=3), dict(ct=-1), dict(bits=16), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(b2=float("nan")), dict(eps=-1.0),
+    for bad in (dict(n=0), dict(n=-1), dict(gt=3), dict(ct=-1), dict(bits=16), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(b2=float("nan")), dict(eps=-1.0), dict(eps=0.0), dict(eps=1e300),
                 dict(eps=inf), dict(step=-1), dict(m=None), dict(v=WS + 8), dict(bits=8), dict(tensors=((P, Q, None, -1, 0.0),)), dict(tensors=((None, Q, None, 5, 0.0),)),
                 dict(tensors=((P, None, None, 5, 0.0),)), dict(tensors=((P + 2, Q, None, 5, 0.0),)), dict(tensors=((P, Q + 1, None, 5, 0.0),)),
                 dict(tensors=((P, Q, None, 5, inf),)),
