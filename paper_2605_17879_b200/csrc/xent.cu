@@ -577,6 +577,7 @@ __device__ __forceinline__ void gather_row(const GatherArgs &a, int64_t r, int a
     const uint4 *from = reinterpret_cast<const uint4 *>((const char *)a.x + r * a.stride * 2);
     uint4 *to = at >= 0 ? reinterpret_cast<uint4 *>(a.to) + (int64_t)at * a.vectors : a.dx ? reinterpret_cast<uint4 *>(a.dx) + r * a.vectors : nullptr;
     if (!to) return;
+#pragma unroll 4
     for (int v = lane_id(); v < a.vectors; v += 32) to[v] = at >= 0 ? from[v] : make_uint4(0, 0, 0, 0);
 }
 // Rows of the gathered copy behind the last one, up to a whole tile: zeros.
@@ -720,14 +721,19 @@ __global__ void __launch_bounds__(256) xent_combine_kernel(const CombineArgs a) 
         }
         const float2 *p = a.parts + r * a.n_parts;
         float top = -INFINITY, sum = 0.0f;
-        for (int i = lane_id(); i < a.n_parts; i += 32) {
-            const float2 q = p[i];
-            const float most = fmaxf(top, q.x), base = finite_or_zero(most);
-            // (nothing summed yet, or an empty part: its exponent says nothing)
-            const float x = sum != 0.0f ? __fmul_rn(sum, exp2_fast(__fmul_rn(__fsub_rn(finite_or_zero(top), base), kLog2e))) : 0.0f;
-            const float y = q.y != 0.0f ? __fmul_rn(q.y, exp2_fast(__fmul_rn(__fsub_rn(finite_or_zero(q.x), base), kLog2e))) : 0.0f;
-            sum = __fadd_rn(x, y);
-            top = most;
+        for (int i = lane_id(); i < a.n_parts; i += 128) {
+            float2 q[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) q[k] = i + 32 * k < a.n_parts ? p[i + 32 * k] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float most = fmaxf(top, q[k].x), base = finite_or_zero(most);
+                // (nothing summed yet, or an empty part: its exponent says nothing)
+                const float x = sum != 0.0f ? __fmul_rn(sum, exp2_fast(__fmul_rn(__fsub_rn(finite_or_zero(top), base), kLog2e))) : 0.0f;
+                const float y = q[k].y != 0.0f ? __fmul_rn(q[k].y, exp2_fast(__fmul_rn(__fsub_rn(finite_or_zero(q[k].x), base), kLog2e))) : 0.0f;
+                sum = __fadd_rn(x, y);
+                top = most;
+            }
         }
         for (int d = 16; d > 0; d >>= 1) {
             const float t2 = __shfl_xor_sync(0xFFFFFFFFu, top, d), s2 = __shfl_xor_sync(0xFFFFFFFFu, sum, d);
@@ -771,6 +777,7 @@ __global__ void __launch_bounds__(256) xent_join_kernel(const JoinArgs a) {
         const int64_t col = tile % a.n_tiles * kN + half * 128 + pair * 8;
         if (col >= a.width) continue;
         float x[8] = {};
+#pragma unroll 4
         for (int k = 0; k < splits; ++k) {
             const float4 *p = a.partial + partial_at(tile * splits + k, rank, half, quarter, pair * 2, lane_id());
             const float4 u = p[0], v = p[32];
