@@ -12,7 +12,8 @@
 //      partial sum: two places a window, in order, so the partial sums are again a sorted list, a sixteenth as long, to which
 //      the same is applied until the list is short; embed_finish_kernel then adds each token's places.  So a token that occurs once costs one read and one write, one that
 //      fills the batch is summed by as many warps as there are windows, and nothing depends on how frequent tokens are.
-//      The first of these launches also writes zeros to the rows whose token is not in the list.
+//      The first of these launches also writes zeros to the rows whose token is not in the list (but for those that the SMs
+//      which had nothing to sort have cleared).
 // The grouping of a sum depends on the positions alone.
 #include "train_ops.h"
 
@@ -161,7 +162,27 @@ struct SortArgs {
     bool scanned;                      // counts hold the numbers before each tile, totals theirs
     int64_t tiles;
     int shift, digits, first;
+    // CTAs behind the sorting ones write zeros meanwhile: a piece of the table's last rows, see launch_embed_grad
+    unsigned sorters;
+    uint8_t *clear;
+    int64_t clear_bytes;
 };
+
+// Zero bytes from p on (a whole number of 2-byte units, aligned to one); `threads` threads together, this one the i-th.
+__device__ __forceinline__ void clear_by(uint8_t *p, int64_t bytes, int64_t i, int64_t threads) {
+    const int64_t head = min(bytes, (int64_t)((16 - ((uintptr_t)p & 15)) & 15));
+    const int64_t vectors = (bytes - head) / 16, done = head + vectors * 16;
+    uint16_t *ends = reinterpret_cast<uint16_t *>(p);
+    uint4 *mid = reinterpret_cast<uint4 *>(p + head);
+    for (int64_t k = i; k < vectors; k += threads) mid[k] = make_uint4(0, 0, 0, 0);
+    for (int64_t k = i; k * 2 < head; k += threads) ends[k] = 0;
+    for (int64_t k = done / 2 + i; k * 2 < bytes; k += threads) ends[k] = 0;
+}
+__device__ __forceinline__ bool clears(const SortArgs &s) {
+    if (blockIdx.x < s.sorters) return false;
+    clear_by(s.clear, s.clear_bytes, (int64_t)(blockIdx.x - s.sorters) * blockDim.x + threadIdx.x, (int64_t)(gridDim.x - s.sorters) * blockDim.x);
+    return true;
+}
 
 __device__ __forceinline__ void load_tile(const SortArgs &s, int64_t tile, uint32_t (&key)[kSortItems], uint32_t (&pos)[kSortItems],
                                           bool (&have)[kSortItems]) {
@@ -183,6 +204,7 @@ __device__ __forceinline__ void load_tile(const SortArgs &s, int64_t tile, uint3
 __global__ void __launch_bounds__(kSortThreads) embed_sort_count_kernel(const SortArgs s) {
     __shared__ uint32_t count[kDigits];
     pdl_wait();
+    if (clears(s)) return;
     count[threadIdx.x] = 0;
     __syncthreads();
     uint32_t key[kSortItems], pos[kSortItems];
@@ -221,6 +243,7 @@ __global__ void __launch_bounds__(1024) embed_sort_scan_kernel(uint32_t *counts,
 __global__ void __launch_bounds__(kSortThreads) embed_sort_move_kernel(const SortArgs s) {
     __shared__ SortShared sh;
     pdl_wait();
+    if (clears(s)) return;
     uint32_t key[kSortItems], pos[kSortItems], rank[kSortItems];
     bool have[kSortItems];
     load_tile(s, blockIdx.x, key, pos, have);
@@ -263,6 +286,7 @@ __global__ void __launch_bounds__(kShortThreads) embed_sort_short_kernel(const S
     ShortShared &sh = *reinterpret_cast<ShortShared *>(dynamic);
     uint32_t *keys = reinterpret_cast<uint32_t *>(reinterpret_cast<uint8_t *>(dynamic) + sizeof(ShortShared)), *places = keys + kItems * kShortThreads;
     pdl_wait();
+    if (clears(s)) return;
     const int lane = lane_id(), warp = warp_id();
     const int at = warp * (32 * kItems) + lane;          // the thread's keys: at, at + 32, ...
     const int n = (int)s.a.n;
@@ -341,7 +365,7 @@ template <int kItems>
 cudaError_t launch_short(const SortArgs &s, cudaStream_t st) {
     constexpr int smem = (int)sizeof(ShortShared) + kItems * kShortThreads * 8;
     const cudaError_t e = cudaFuncSetAttribute(embed_sort_short_kernel<kItems>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    return e != cudaSuccess ? e : launch_after_smem(embed_sort_short_kernel<kItems>, dim3(1), dim3(kShortThreads), smem, st, s);
+    return e != cudaSuccess ? e : launch_after_smem(embed_sort_short_kernel<kItems>, dim3(s.clear_bytes ? (unsigned)sm_count() : 1u), dim3(kShortThreads), smem, st, s);
 }
 
 // ---- sums ------------------------------------------------------------------------------------------------------------
@@ -358,11 +382,15 @@ struct List {
 
 struct SumArgs {
     List list;                   // sorted keys (kHole: nothing there)
-    int64_t rows, width;
+    int64_t rows, width, clear_to;   // rows from clear_to on are zero already
     float scale;
     int accumulate;
     void *dtable;
-    unsigned sum_blocks, clear_blocks;   // clear_blocks (first list only): write zeros to the rows without tokens
+    const uint32_t *all_key;     // the first list, for the CTAs that write zeros to the rows without tokens
+    int64_t all_n;
+    bool clear_late;             // those are in the last launch, not in the first
+    int clear_each;
+    unsigned sum_blocks, clear_blocks;
     int strips;
 };
 
@@ -422,27 +450,16 @@ __device__ __forceinline__ int64_t warp_lower_bound(const uint32_t *key, int64_t
     return lo;
 }
 
-// Zero bytes from p on (a whole number of elements, aligned to one); the warp together, vectors of 16 bytes in between.
-__device__ __forceinline__ void clear_stretch(uint8_t *p, int64_t bytes) {
-    const int64_t head = min(bytes, (int64_t)((16 - ((uintptr_t)p & 15)) & 15));
-    uint16_t *ends = reinterpret_cast<uint16_t *>(p);
-    for (int64_t i = lane_id(); i * 2 < head; i += 32) ends[i] = 0;
-    const int64_t vectors = (bytes - head) / 16;
-    uint4 *mid = reinterpret_cast<uint4 *>(p + head);
-    for (int64_t i = lane_id(); i < vectors; i += 32) mid[i] = make_uint4(0, 0, 0, 0);
-    const int64_t done = head + vectors * 16;
-    for (int64_t i = done / 2 + lane_id(); i * 2 < bytes; i += 32) ends[i] = 0;
-}
-
-// Zeros for the rows of the table without tokens, 32 rows a warp: the sorted keys say which those are.
+// Zeros for the rows of the table without tokens, clear_each rows a warp (at most 32): the sorted keys say which those are.
 template <typename O>
 __device__ __forceinline__ void clear_rows(const SumArgs &s, int64_t warp, int64_t warps) {
     O *table = reinterpret_cast<O *>(s.dtable);
-    const uint32_t *key = s.list.key;
-    const int64_t n = s.list.n;
-    for (int64_t first = warp * 32; first < s.rows; first += warps * 32) {
+    const uint32_t *key = s.all_key;
+    const int64_t n = s.all_n;
+    for (int64_t first = warp * s.clear_each; first < s.clear_to; first += warps * s.clear_each) {
+        const int64_t last = min(first + s.clear_each, s.clear_to);
         int64_t lo = warp_lower_bound(key, n, (uint32_t)first);
-        const int64_t end = lo + warp_lower_bound(key + lo, n - lo, (uint32_t)min(first + 32, s.rows));
+        const int64_t end = lo + warp_lower_bound(key + lo, n - lo, (uint32_t)last);
         const int64_t mine = first + lane_id();
         int64_t hi = end;
         while (lo < hi) {                             // the lane's own row among those
@@ -450,13 +467,13 @@ __device__ __forceinline__ void clear_rows(const SumArgs &s, int64_t warp, int64
             if (key[mid] < (uint32_t)mine) lo = mid + 1;
             else hi = mid;
         }
-        const bool empty = mine < s.rows && !(lo < end && key[lo] == (uint32_t)mine);
+        const bool empty = mine < last && !(lo < end && key[lo] == (uint32_t)mine);
         uint32_t rows = __ballot_sync(0xFFFFFFFFu, empty);
         while (rows) {                                // runs of them are one stretch of memory each
             const int at = __ffs(rows) - 1;
             const int run = __ffs(~(rows >> at) | (at ? 1u << (32 - at) : 0u)) - 1;      // (ends at row 32)
             const int count = run < 0 ? 32 : run;
-            clear_stretch(reinterpret_cast<uint8_t *>(table + (first + at) * s.width), (int64_t)count * s.width * sizeof(O));
+            clear_by(reinterpret_cast<uint8_t *>(table + (first + at) * s.width), (int64_t)count * s.width * sizeof(O), lane_id(), 32);
             rows = at + count >= 32 ? 0u : rows & ~((1u << (at + count)) - 1);
         }
     }
@@ -564,6 +581,11 @@ __global__ void __launch_bounds__(kFinishThreads) embed_finish_kernel(const SumA
     __shared__ int count;
     if (threadIdx.x == 0) count = 0;
     pdl_wait();
+    if (blockIdx.x >= s.strips) {
+        constexpr int kWarps = kFinishThreads / 32;
+        clear_rows<O>(s, (int64_t)(blockIdx.x - s.strips) * kWarps + warp_id(), (int64_t)(gridDim.x - s.strips) * kWarps);
+        return;
+    }
     const int n = (int)s.list.n, i = threadIdx.x;
     keys[i] = i < n ? s.list.key[i] : 0xFFFFFFFFu;
     __syncthreads();
@@ -639,7 +661,7 @@ cudaError_t launch_sum(SumArgs s, bool first, bool wide, cudaStream_t st) {
     int64_t blocks = (work + kSumWarps - 1) / kSumWarps;
     if (blocks > most * 16) blocks = most * 16;
     s.sum_blocks = (unsigned)blocks;
-    int64_t clear = first && !s.accumulate ? (s.rows + 32 * kSumWarps - 1) / (32 * kSumWarps) : 0;
+    int64_t clear = first && !s.accumulate && !s.clear_late ? (s.clear_to + s.clear_each * kSumWarps - 1) / (s.clear_each * kSumWarps) : 0;
     if (clear > most * 4) clear = most * 4;
     s.clear_blocks = (unsigned)clear;
     if (blocks + clear == 0) return cudaSuccess;
@@ -657,7 +679,10 @@ cudaError_t launch_sums(SumArgs s, const GradLayout &L, char *ws, bool wide, cud
         s.list.next = next ? (float *)(ws + L.next[to]) : nullptr;
         cudaError_t e;
         if (level > 0 && s.list.n <= kFinish) {
-            const dim3 grid((unsigned)((s.width + 127) / 128)), block(kFinishThreads);
+            s.strips = (int)((s.width + 127) / 128);
+            int64_t clear = s.clear_late && !s.accumulate ? (s.clear_to * 32 + kFinishThreads * s.clear_each - 1) / (kFinishThreads * s.clear_each) : 0;
+            if (clear > sm_count() * 4) clear = sm_count() * 4;
+            const dim3 grid((unsigned)(s.strips + clear)), block(kFinishThreads);
             return wide ? launch_after(embed_finish_kernel<T, true>, grid, block, st, s) : launch_after(embed_finish_kernel<T, false>, grid, block, st, s);
         }
         e = level == 0 ? launch_sum<T, T>(s, true, wide, st) : launch_sum<float, T>(s, false, wide, st);
@@ -665,6 +690,9 @@ cudaError_t launch_sums(SumArgs s, const GradLayout &L, char *ws, bool wide, cud
         s.list = List{next, s.list.next_key, nullptr, s.list.next, s.width, nullptr, nullptr};
     }
 }
+
+// Bytes that all SMs clear while one CTA sorts up to 1 024 keys (5 us) or 8 192 (18 us), and per launch of longer sorts.
+constexpr int64_t kTinyClear = 16 << 20, kShortClear = 64 << 20, kLaunchClear = 20 << 20;
 
 bool aligned(const void *p, size_t to) { return (uintptr_t)p % to == 0; }
 
@@ -700,13 +728,37 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
     s.digits = (bits + kDigitBits - 1) / kDigitBits;
     int at = 0;      // which of the two orders holds the result
     cudaError_t e;
+    // Writing the table, at 3.9 TB/s as a memset does, is what bounds the whole, and sorting needs few SMs.  So the others
+    // write zeros to the last rows meanwhile, as much as takes as long as the sort; rows whose token occurs are written again
+    // later.  What is left is cleared beside the first sums, or, for short lists, whose few reads would wait behind the writes,
+    // beside the last ones.  5 003 x 1 001 into 32 001 rows of float32: 48 us so, 52 beside the first, 62 without a head start.
+    const int64_t sms = sm_count(), row_bytes = a.width * (int64_t)dtype_bytes(dtype);
+    const bool is_short = a.n <= 8 * kShortThreads;
+    const int64_t spare = is_short ? sms - 1 : sms - L.tiles, launches = is_short ? 1 : 2 * s.digits;
+    int64_t early = 0;                   // rows
+    if (!a.accumulate && spare > sms / 4) {
+        const int64_t bytes = (!is_short ? kLaunchClear * launches : a.n > kShortThreads ? kShortClear : kTinyClear) * spare / sms;
+        early = bytes / row_bytes < a.rows ? bytes / row_bytes : a.rows;
+    }
+    uint8_t *const early_from = (uint8_t *)a.dtable + (a.rows - early) * row_bytes;
+    int64_t given = 0;
+    auto share = [&](int64_t launch) {   // of the launch-th: whole rows
+        const int64_t to = early * (launch + 1) / launches;
+        s.clear = early_from + given * row_bytes;
+        s.clear_bytes = (to - given) * row_bytes;
+        given = to;
+    };
     // one CTA sorts 8 192 keys in 14 us, the launches per digit that many more take 23
-    if (a.n <= 8 * kShortThreads) {
+    if (is_short) {
+        s.sorters = 1;
+        share(0);
         s.out_key = (uint32_t *)(ws + L.key[0]);
         s.out_pos = (uint32_t *)(ws + L.pos[0]);
         e = a.n <= kShortThreads ? launch_short<1>(s, st) : a.n <= 2 * kShortThreads ? launch_short<2>(s, st) : a.n <= 4 * kShortThreads ? launch_short<4>(s, st) : launch_short<8>(s, st);
         if (e != cudaSuccess) return e;
     } else {
+        s.sorters = (unsigned)L.tiles;
+        const unsigned grid = (unsigned)(L.tiles + (early ? spare : 0));
         for (int d = 0; d < s.digits; ++d) {
             s.first = d == 0;
             s.shift = d * kDigitBits;
@@ -715,18 +767,25 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
             if (d > 0) at ^= 1;
             s.out_key = (uint32_t *)(ws + L.key[at]);
             s.out_pos = (uint32_t *)(ws + L.pos[at]);
-            e = launch_after(embed_sort_count_kernel, dim3((unsigned)L.tiles), dim3(kSortThreads), st, s);
+            share(2 * d);
+            e = launch_after(embed_sort_count_kernel, dim3(grid), dim3(kSortThreads), st, s);
             if (e != cudaSuccess) return e;
             // (each CTA of the move adds the counts of all tiles up itself where they are few)
             s.scanned = L.tiles > 64;
             if (s.scanned) e = launch_after(embed_sort_scan_kernel, dim3(kDigits / 32), dim3(1024), st, s.counts, L.tiles);
             if (e != cudaSuccess) return e;
-            e = launch_after(embed_sort_move_kernel, dim3((unsigned)L.tiles), dim3(kSortThreads), st, s);
+            share(2 * d + 1);
+            e = launch_after(embed_sort_move_kernel, dim3(grid), dim3(kSortThreads), st, s);
             if (e != cudaSuccess) return e;
         }
     }
     SumArgs u{};
     u.list = List{a.n, (const uint32_t *)(ws + L.key[at]), (const uint32_t *)(ws + L.pos[at]), a.grad, a.stride, nullptr, nullptr};
+    u.clear_to = a.rows - early;
+    u.all_key = u.list.key;
+    u.all_n = a.n;
+    u.clear_late = is_short && a.n > kShortThreads;
+    u.clear_each = u.clear_to > sms * 16 * 32 ? 32 : 8;      // enough warps to use every SM
     u.rows = a.rows;
     u.width = a.width;
     u.scale = a.scale;
