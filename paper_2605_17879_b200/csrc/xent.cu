@@ -11,11 +11,10 @@
 // backward pass computes the logits again, a piece of the vocabulary at a time), or a gradient.
 //
 // Bound: the tensor cores, 2 N V D operations per product, but for few rows, where reading w once is what takes the time.
-// That forward pass takes 426 us, 1 290 TFLOP/s.  The tensor cores are busy four fifths of it: without loads or without the
-// reading warps' work the same products run at 1 450, with neither at 1 560 TFLOP/s.  Those warps share the shared-memory pipe
-// with the operands, so what they do to memory counts: an array that the compiler put there, and rows of results that were
-// stored 16 bytes a lane instead of by TMA, cost 70 us.  Long runs of large products are bound by the power limit
-// (8 192 x 4 096 x 131 072 with gradients, four products: 27 to 29 ms, 1 220 to 1 300 TFLOP/s).
+// That product alone takes 328 us, 1 677 TFLOP/s (tensor cores busy 89 % of the cycles); pass after pass 426 us, since the
+// power limit lowers the clock, as it does for all large sizes (8 192 x 4 096 x 131 072 with gradients, four products: 27 to
+// 29 ms, 1 220 to 1 300 TFLOP/s).  The reading warps share the shared-memory pipe with the operands, so what they do to memory
+// counts: an array that the compiler put there, and rows of results stored 16 bytes a lane instead of by TMA, cost 70 us.
 //
 // Rounding: G is held in the inputs' type, since the tensor cores take both operands in one type; each value is off by at
 // most half a step (relative), as independent of its neighbours as the outputs' own rounding.  It is held relative to the
@@ -252,7 +251,7 @@ __device__ __forceinline__ float pick(int j, int at, float y, float z) {
 // LONG: the depth takes more than one pass.  The tensor cores cut off what an accumulator's last bit cannot hold, product
 // step by product step, which shrinks a logit by some 2^-24 a step; the forward pass, whose results are float32, starts a new
 // accumulator every kPass stages and adds them in registers, rounded to nearest: the losses of 4 096 deep logits are off by
-// less than 1e-6 of themselves so, and by more without.  G, which is rounded to 16 bits, does not need it.
+// 3.4e-7 of themselves so, as those of 1 024 deep ones are, and by over 1e-6 without.  G, rounded to 16 bits, can do without.
 template <int MODE, bool LONG, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1) __cluster_dims__(2, 1, 1)
 product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ ProductArgs a) {
