@@ -7,7 +7,7 @@
 // the order, and with it the result, a matter of chance, and would serialise on frequent tokens; so the positions are sorted
 // by token first (a stable radix sort), and runs of one token are summed.
 //   1. embed_sort_*: least significant digit first, kDigitBits at a time; a CTA ranks a tile of keys with warp matches and
-//      counters of its own, so equal keys keep their order.  Short lists: all digits in one launch.  Others: two launches per digit.
+//      counters of its own, so equal keys keep their order; two launches per digit.  Short lists: every key's place counted directly.
 //   2. embed_sum_kernel: a warp takes a window of 32 sorted positions and a strip of columns, loads eight rows' vectors at a
 //      time and adds them run by run.  A run inside the window is a finished row.  One that crosses its borders leaves a
 //      partial sum: two places a window, in order, so the partial sums are again a sorted list, a sixteenth as long, to which
@@ -95,9 +95,8 @@ struct SortShared {
     uint32_t scan[kSortWarps];
 };
 
-// A position's key: its token, or `rows` (behind all tokens) where it adds nothing.
-__device__ __forceinline__ uint32_t key_at(const EmbedGradArgs &a, int64_t i) {
-    const int64_t t = token_at(a.tokens, a.token_bits, i);
+// A token's key: the token, or `rows` (behind all tokens) where it adds nothing.
+__device__ __forceinline__ uint32_t key_of(const EmbedGradArgs &a, int64_t t) {
     if (t == a.padding) return (uint32_t)a.rows;
     if (t < 0 || t >= a.rows) {
         if (a.status) atomicOr(a.status, kStatIndex);
@@ -105,6 +104,7 @@ __device__ __forceinline__ uint32_t key_at(const EmbedGradArgs &a, int64_t i) {
     }
     return (uint32_t)t;
 }
+__device__ __forceinline__ uint32_t key_at(const EmbedGradArgs &a, int64_t i) { return key_of(a, token_at(a.tokens, a.token_bits, i)); }
 
 // Ranks the tile's keys by a digit.  Thread holds kSortItems keys, warp after warp and 32 at a time in order, so that rank
 // order is position order.  rank[r]: number of keys of the same digit before this one in the warp; counts per warp in s.count.
@@ -276,99 +276,61 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_move_kernel(const Sor
         }
 }
 
-// Short lists: every digit in turn by one CTA of 1 024 threads, kItems keys each, in shared memory.
-constexpr int kShortThreads = 1024, kShortWarps = kShortThreads / 32;
-struct ShortShared {
-    alignas(16) uint16_t count[kShortWarps][kDigits];
-    uint32_t base[kDigits];
-    uint32_t scan[kShortWarps];
-};
-template <int kItems>
-__global__ void __launch_bounds__(kShortThreads) embed_sort_short_kernel(const SortArgs s) {
-    extern __shared__ uint4 dynamic[];
-    ShortShared &sh = *reinterpret_cast<ShortShared *>(dynamic);
-    uint32_t *keys = reinterpret_cast<uint32_t *>(reinterpret_cast<uint8_t *>(dynamic) + sizeof(ShortShared)), *places = keys + kItems * kShortThreads;
+// Short lists: a key's place is the number of keys that come before it, and counting them all is quick: a CTA holds the list
+// in shared memory and counts for 64 of its keys, four a warp, 128 comparisons with each at a time.  5 003 keys: 12 us, where
+// one CTA took 18 for the digits in turn.
+constexpr int kShort = 8192, kRankThreads = 512, kRankEach = 64;
+__global__ void __launch_bounds__(kRankThreads) embed_sort_short_kernel(const SortArgs s) {
+    __shared__ alignas(16) uint32_t keys[kShort];
     pdl_wait();
     if (clears(s)) return;
-    const int lane = lane_id(), warp = warp_id();
-    const int at = warp * (32 * kItems) + lane;          // the thread's keys: at, at + 32, ...
-    const int n = (int)s.a.n;
-    uint32_t key[kItems], pos[kItems], rank[kItems];
+    const int n = (int)s.a.n, blocks = (n + 127) / 128, lane = lane_id();
+    for (int j0 = threadIdx.x; j0 < blocks * 128; j0 += kRankThreads * 8) {
+        int64_t t[8];                    // (all on their way before the first is looked at)
 #pragma unroll
-    for (int r = 0; r < kItems; ++r) {
-        const int i = at + r * 32;
-        key[r] = i < n ? key_at(s.a, i) : 0;
-        pos[r] = i;
+        for (int k = 0; k < 8; ++k) t[k] = j0 + k * kRankThreads < n ? token_at(s.a.tokens, s.a.token_bits, j0 + k * kRankThreads) : 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int j = j0 + k * kRankThreads;
+            if (j < blocks * 128) keys[j] = j < n ? key_of(s.a, t[k]) : 0xFFFFFFFFu;
+        }
     }
-    for (int d = 0; d < s.digits; ++d) {
-        const int shift = d * kDigitBits;
-        for (int i = threadIdx.x; i < kShortWarps * kDigits / 8; i += kShortThreads) reinterpret_cast<uint4 *>(&sh.count[0][0])[i] = make_uint4(0, 0, 0, 0);
-        __syncthreads();
+    __syncthreads();
+    constexpr int kMine = kRankEach / (kRankThreads / 32);
+    const int i0 = blockIdx.x * kRankEach + warp_id() * kMine;
+    if (i0 >= n) return;
+    uint32_t key[kMine], count[kMine] = {};
 #pragma unroll
-        for (int r = 0; r < kItems; ++r) {               // (as rank_tile)
-            const bool have = at + r * 32 < n;
-            const uint32_t digit = have ? (key[r] >> shift) & (kDigits - 1) : kDigits;
-            const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
-            const int first = __ffs(same) - 1;
-            uint32_t before = 0;
-            if (lane == first && have) {
-                before = sh.count[warp][digit];
-                sh.count[warp][digit] = (uint16_t)(before + __popc(same));
-            }
-            before = __shfl_sync(0xFFFFFFFFu, before, first);
-            rank[r] = before + __popc(same & ((1u << lane) - 1));
-            __syncwarp();
-        }
-        __syncthreads();
-        // numbers before each warp, then before each digit
-        uint32_t mine = 0;
-        if (threadIdx.x < kDigits) {
-#pragma unroll 8
-            for (int w = 0; w < kShortWarps; ++w) {
-                const uint32_t c = sh.count[w][threadIdx.x];
-                sh.count[w][threadIdx.x] = (uint16_t)mine;
-                mine += c;
-            }
-        }
-        uint32_t upto = mine;
-        for (int k = 1; k < 32; k <<= 1) {
-            const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, upto, k);
-            if (lane >= k) upto += y;
-        }
-        if (lane == 31) sh.scan[warp] = upto;
-        __syncthreads();
-        if (threadIdx.x < kDigits) sh.base[threadIdx.x] = upto - mine + __reduce_add_sync(0xFFFFFFFFu, lane < warp ? sh.scan[lane] : 0u);
-        __syncthreads();
+    for (int m = 0; m < kMine; ++m) key[m] = keys[min(i0 + m, n - 1)];
+    for (int b = 0; b < blocks; ++b) {
+        const uint4 k = reinterpret_cast<const uint4 *>(keys)[b * 32 + lane];
+        const uint32_t other[4] = {k.x, k.y, k.z, k.w};
+        // before: smaller, or equal and further ahead in the list
+        if (b * 128 + 128 <= i0) {
 #pragma unroll
-        for (int r = 0; r < kItems; ++r)
-            if (at + r * 32 < n) {
-                const uint32_t digit = (key[r] >> shift) & (kDigits - 1);
-                const uint32_t to = sh.base[digit] + sh.count[warp][digit] + rank[r];
-                keys[to] = key[r];
-                places[to] = pos[r];
-            }
-        __syncthreads();
+            for (int m = 0; m < kMine; ++m)
 #pragma unroll
-        for (int r = 0; r < kItems; ++r)
-            if (at + r * 32 < n) {
-                key[r] = keys[at + r * 32];
-                pos[r] = places[at + r * 32];
-            }
-        // (the next digit's counters are cleared, and its keys written, after barriers that follow these reads)
+                for (int e = 0; e < 4; ++e) count[m] += other[e] <= key[m];
+        } else if (b * 128 >= i0 + kMine) {
+#pragma unroll
+            for (int m = 0; m < kMine; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) count[m] += other[e] < key[m];
+        } else {
+#pragma unroll
+            for (int m = 0; m < kMine; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) count[m] += other[e] < key[m] || (other[e] == key[m] && b * 128 + lane * 4 + e < i0 + m);
+        }
     }
 #pragma unroll
-    for (int r = 0; r < kItems; ++r)
-        if (at + r * 32 < n) {
-            s.out_key[at + r * 32] = key[r];
-            s.out_pos[at + r * 32] = pos[r];
+    for (int m = 0; m < kMine; ++m) {
+        const uint32_t to = __reduce_add_sync(0xFFFFFFFFu, count[m]);
+        if (lane == 0 && i0 + m < n) {
+            s.out_key[to] = key[m];
+            s.out_pos[to] = (uint32_t)(i0 + m);
         }
-}
-
-template <int kItems>
-cudaError_t launch_short(const SortArgs &s, cudaStream_t st) {
-    constexpr int smem = (int)sizeof(ShortShared) + kItems * kShortThreads * 8;
-    const cudaError_t e = cudaFuncSetAttribute(embed_sort_short_kernel<kItems>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    return e != cudaSuccess ? e : launch_after_smem(embed_sort_short_kernel<kItems>, dim3(s.clear_bytes ? (unsigned)sm_count() : 1u), dim3(kShortThreads), smem, st, s);
+    }
 }
 
 // ---- sums ------------------------------------------------------------------------------------------------------------
@@ -694,7 +656,8 @@ cudaError_t launch_sums(SumArgs s, const GradLayout &L, char *ws, bool wide, cud
     }
 }
 
-// Bytes that all SMs clear while one CTA sorts up to 1 024 keys (5 us) or 8 192 (18 us), and per launch of longer sorts.
+// Bytes that are cleared beside the sort of up to kFew keys, of a short list, and in each launch of longer sorts.
+constexpr int kFew = 1024;
 constexpr int64_t kTinyClear = 16 << 20, kShortClear = 64 << 20, kLaunchClear = 20 << 20;
 
 bool aligned(const void *p, size_t to) { return (uintptr_t)p % to == 0; }
@@ -731,16 +694,16 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
     s.digits = (bits + kDigitBits - 1) / kDigitBits;
     int at = 0;      // which of the two orders holds the result
     cudaError_t e;
-    // Writing the table, at 3.9 TB/s as a memset does, is what bounds the whole, and sorting needs few SMs.  So the others
-    // write zeros to the last rows meanwhile, as much as takes as long as the sort; rows whose token occurs are written again
+    // Writing the table, at 3.9 TB/s as a memset does, is what bounds the whole, and sorting does not use memory.  So other CTAs
+    // write zeros to the last rows meanwhile; rows whose token occurs are written again
     // later.  What is left is cleared beside the first sums, or, for short lists, whose few reads would wait behind the writes,
-    // beside the last ones.  5 003 x 1 001 into 32 001 rows of float32: 48 us so, 52 beside the first, 62 without a head start.
+    // beside the last ones.  5 003 x 1 001 into 32 001 rows of float32: 45 us so; 48, 52 beside the first and 62 without a head start while one CTA sorted.
     const int64_t sms = sm_count(), row_bytes = a.width * (int64_t)dtype_bytes(dtype);
-    const bool is_short = a.n <= 8 * kShortThreads;
-    const int64_t spare = is_short ? sms - 1 : sms - L.tiles, launches = is_short ? 1 : 2 * s.digits;
+    const bool is_short = a.n <= kShort;
+    const int64_t spare = is_short ? sms : sms - L.tiles, launches = is_short ? 1 : 2 * s.digits;
     int64_t early = 0;                   // rows
     if (!a.accumulate && spare > sms / 4) {
-        const int64_t bytes = (!is_short ? kLaunchClear * launches : a.n > kShortThreads ? kShortClear : kTinyClear) * spare / sms;
+        const int64_t bytes = (!is_short ? kLaunchClear * launches : a.n > kFew ? kShortClear : kTinyClear) * spare / sms;
         early = bytes / row_bytes < a.rows ? bytes / row_bytes : a.rows;
     }
     uint8_t *const early_from = (uint8_t *)a.dtable + (a.rows - early) * row_bytes;
@@ -751,13 +714,13 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
         s.clear_bytes = (to - given) * row_bytes;
         given = to;
     };
-    // one CTA sorts 8 192 keys in 14 us, the launches per digit that many more take 23
     if (is_short) {
-        s.sorters = 1;
+        s.sorters = (unsigned)((a.n + kRankEach - 1) / kRankEach);
         share(0);
         s.out_key = (uint32_t *)(ws + L.key[0]);
         s.out_pos = (uint32_t *)(ws + L.pos[0]);
-        e = a.n <= kShortThreads ? launch_short<1>(s, st) : a.n <= 2 * kShortThreads ? launch_short<2>(s, st) : a.n <= 4 * kShortThreads ? launch_short<4>(s, st) : launch_short<8>(s, st);
+        const int64_t grid = s.sorters + (early ? sms : 0);
+        e = grid ? launch_after(embed_sort_short_kernel, dim3((unsigned)grid), dim3(kRankThreads), st, s) : cudaSuccess;
         if (e != cudaSuccess) return e;
     } else {
         s.sorters = (unsigned)L.tiles;
@@ -787,7 +750,7 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
     u.clear_to = a.rows - early;
     u.all_key = u.list.key;
     u.all_n = a.n;
-    u.clear_late = is_short && a.n > kShortThreads;
+    u.clear_late = is_short && a.n > kFew;
     u.clear_each = u.clear_to > sms * 16 * 32 ? 32 : 8;      // enough warps to use every SM
     u.rows = a.rows;
     u.width = a.width;
