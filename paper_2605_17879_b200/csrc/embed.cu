@@ -697,7 +697,8 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
     // Writing the table, at 3.9 TB/s as a memset does, is what bounds the whole, and sorting does not use memory.  So other CTAs
     // write zeros to the last rows meanwhile; rows whose token occurs are written again
     // later.  What is left is cleared beside the first sums, or, for short lists, whose few reads would wait behind the writes,
-    // beside the last ones.  5 003 x 1 001 into 32 001 rows of float32: 45 us so; 48, 52 beside the first and 62 without a head start while one CTA sorted.
+    // beside the last ones.  5 003 x 1 001 into 32 001 rows of float32: 45 us (with another sort: 48 so, 52 with the rest beside
+    // the first sums, 62 without a head start).
     const int64_t sms = sm_count(), row_bytes = a.width * (int64_t)dtype_bytes(dtype);
     const bool is_short = a.n <= kShort;
     const int64_t spare = is_short ? sms : sms - L.tiles, launches = is_short ? 1 : 2 * s.digits;
