@@ -41,7 +41,7 @@ constexpr int kHalf = 128;                    // rows of either operand that eac
 constexpr int kStages = 6;
 constexpr int kOperand = kHalf * kK * 2;      // bytes
 constexpr int kStage = 2 * kOperand;
-constexpr int kPass = 1024 / kK;              // stages that one accumulator takes in the forward pass
+constexpr int kPass = 1024 / kK;              // stages of a logit that one accumulator takes
 constexpr int kEpilogueWarps = 8;
 constexpr int kProductThreads = 32 * (4 + kEpilogueWarps);
 constexpr int kBox = 32 * 128;                // bytes of what a warp stores at a time: 32 rows of 64 values
@@ -197,22 +197,23 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) 
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// 32 values of a thread's row to 16-bit memory, those before `left` (a multiple of eight).
-template <typename T>
-__device__ __forceinline__ void store_row32(T *p, int left, const float (&x)[32]) {
+// N values of a thread's row to 16-bit memory, those before `left` (a multiple of eight).
+template <typename T, int N>
+__device__ __forceinline__ void store_row(T *p, int left, const float (&x)[N]) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < N / 8; ++q)
         if (8 * q < left)
             reinterpret_cast<uint4 *>(p)[q] = make_uint4(pack2<T>(x[8 * q], x[8 * q + 1]), pack2<T>(x[8 * q + 2], x[8 * q + 3]),
                                                          pack2<T>(x[8 * q + 4], x[8 * q + 5]), pack2<T>(x[8 * q + 6], x[8 * q + 7]));
 }
-// 32 values of a thread's row to half `h` of the warp's box in shared memory (32 rows of 128 bytes, swizzled as TMA wants).
-template <typename T>
-__device__ __forceinline__ void box_row32(uint8_t *box, int h, const float (&x)[32]) {
+// N values of a thread's row to the h-th place for so many in the warp's box in shared memory (32 rows of 128 bytes, swizzled
+// as TMA wants).
+template <typename T, int N>
+__device__ __forceinline__ void box_row(uint8_t *box, int h, const float (&x)[N]) {
     const int row = lane_id();
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<uint4 *>(box + row * 128 + (((h * 4 + q) ^ (row & 7)) << 4)) =
+    for (int q = 0; q < N / 8; ++q)
+        *reinterpret_cast<uint4 *>(box + row * 128 + (((h * (N / 8) + q) ^ (row & 7)) << 4)) =
             make_uint4(pack2<T>(x[8 * q], x[8 * q + 1]), pack2<T>(x[8 * q + 2], x[8 * q + 3]), pack2<T>(x[8 * q + 4], x[8 * q + 5]),
                        pack2<T>(x[8 * q + 6], x[8 * q + 7]));
 }
@@ -249,9 +250,10 @@ __device__ __forceinline__ float pick(int j, int at, float y, float z) {
 }
 
 // LONG: the depth takes more than one pass.  The tensor cores cut off what an accumulator's last bit cannot hold, product
-// step by product step, which shrinks a logit by some 2^-24 a step; the forward pass, whose results are float32, starts a new
-// accumulator every kPass stages and adds them in registers, rounded to nearest: the losses of 4 096 deep logits are off by
-// 3.4e-7 of themselves so, as those of 1 024 deep ones are, and by over 1e-6 without.  G, rounded to 16 bits, can do without.
+// step by product step, which shrinks a logit by some 2^-24 a step; so logits start a new accumulator every kPass stages and
+// add them in registers, rounded to nearest: the losses of 4 096 deep logits are off by 3.4e-7 of themselves so, as those of
+// 1 024 deep ones are, and by over 1e-6 without.  The backward pass takes the same steps, so that its logits are the forward
+// pass's to the last bit: where a target has all the probability, G is exp(z - lse) - 1 = 0 only if lse was made of this z.
 template <int MODE, bool LONG, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1) __cluster_dims__(2, 1, 1)
 product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ ProductArgs a) {
@@ -384,13 +386,14 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
             const int row = u.m * kM + rank * kHalf + quarter * 32 + lane;
             const bool empty = u.k0 == u.k1;       // no depth at all: the accumulator was not written
             int64_t target = -1;
-            float lse2 = 0.0f, g = 0.0f;
+            float lse = 0.0f, lse2 = 0.0f, g = 0.0f;
             if (MODE == kStats || MODE == kGrad) {
                 if (row < rows) {
                     if (a.target) target = a.target[row];
                     else target = a.target_bits == 64 ? reinterpret_cast<const long long *>(a.raw_target)[row] : reinterpret_cast<const int *>(a.raw_target)[row];
                     if (MODE == kGrad) {
-                        lse2 = __fmul_rn(a.lse[row], kLog2e);
+                        lse = a.lse[row];
+                        lse2 = __fmul_rn(lse, kLog2e);
                         g = __fmul_rn(__fdiv_rn(a.grad[row], unit), scale);
                     }
                 }
@@ -468,36 +471,49 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
                 const int64_t most = MODE == kGrad ? INT64_MAX : dx ? rows : a.vocab - a.v0;      // rows that are there
                 const int64_t left = MODE == kGrad ? a.vocab - a.v0 - col0 : a.width - col0;     // columns that are there
                 const int at = (int)max((int64_t)-1, min((int64_t)128, target - a.v0 - col0));
-#pragma unroll 1
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t r[32];
-                    float x[32];
-                    tmem_load32(from + c * 32, r);
+                constexpr int N = LONG ? 16 : 32, kSteps = 128 / N, kBoxSteps = 64 / N;
+                constexpr int kUnroll = LONG ? kSteps : 1;
+#pragma unroll kUnroll
+                for (int c = 0; c < kSteps; ++c) {
+                    uint32_t r[N];
+                    float x[N];
+                    if constexpr (LONG) tmem_load16(from + c * N, r);
+                    else tmem_load32(from + c * N, r);
                     tmem_load_wait();
-                    if (c == 3) {
+                    if (c == kSteps - 1) {
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive_at(freed);
                     }
                     if constexpr (MODE == kGrad) {
+                        const bool here = at >= c * N && at < (c + 1) * N;
+                        float y = 0.0f;                                  // the target's logit
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) x[j] = __fmul_rn(exp2_fast(__fmaf_rn(__uint_as_float(r[j]), kLog2e, -lse2)), g);
-                        const bool here = at >= c * 32 && at < (c + 1) * 32;
-                        if (__any_sync(0xFFFFFFFFu, here)) {             // the target: less one
+                        for (int j = 0; j < N; ++j) {
+                            x[j] = __uint_as_float(r[j]);
+                            if constexpr (LONG) x[j] = __fadd_rn(held[c * N + j], x[j]);
+                        }
+                        if (__any_sync(0xFFFFFFFFu, here)) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                x[j] = pick(c * 32 + j, at, __fmul_rn(__fsub_rn(exp2_fast(__fmaf_rn(__uint_as_float(r[j]), kLog2e, -lse2)), 1.0f), g), x[j]);
+                            for (int j = 0; j < N; ++j) y = pick(c * N + j, at, x[j], y);
+                        }
+#pragma unroll
+                        for (int j = 0; j < N; ++j) x[j] = __fmul_rn(exp2_fast(__fmaf_rn(x[j], kLog2e, -lse2)), g);
+                        if (__any_sync(0xFFFFFFFFu, here)) {             // the target: less one, which may leave little
+                            y = __fmul_rn(expm1f(__fsub_rn(y, lse)), g);
+#pragma unroll
+                            for (int j = 0; j < N; ++j) x[j] = pick(c * N + j, at, y, x[j]);
                         }
                         // (G has whole tiles: its padding is written as zeros)
-                        if (left < (c + 1) * 32 || row >= rows) {
+                        if (left < (c + 1) * N || row >= rows) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (c * 32 + j >= left || row >= rows) x[j] = 0.0f;
+                            for (int j = 0; j < N; ++j)
+                                if (c * N + j >= left || row >= rows) x[j] = 0.0f;
                         }
                     } else if (partly) {
 #pragma unroll
-                        for (int q = 0; q < 8; ++q) {
-                            float4 *p = a.partial + partial_at(u.place, rank, half, quarter, c * 8 + q, lane);
+                        for (int q = 0; q < N / 4; ++q) {
+                            float4 *p = a.partial + partial_at(u.place, rank, half, quarter, c * (N / 4) + q, lane);
                             float4 y = make_float4(__uint_as_float(r[4 * q]), __uint_as_float(r[4 * q + 1]), __uint_as_float(r[4 * q + 2]), __uint_as_float(r[4 * q + 3]));
                             if (empty) y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                             if (a.add) {
@@ -509,25 +525,26 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
                         continue;
                     } else {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) x[j] = empty ? 0.0f : __fmul_rn(__uint_as_float(r[j]), inverse);
+                        for (int j = 0; j < N; ++j) x[j] = empty ? 0.0f : __fmul_rn(__uint_as_float(r[j]), inverse);
                     }
                     if (boxes) {
-                        if ((c & 1) == 0) {          // the box's memory, once the last store has read it
+                        if (c % kBoxSteps == 0) {    // the box's memory, once the last store has read it
                             if (lane == 0) tma_store_wait_read();
                             __syncwarp();
                         }
-                        box_row32<T>(box, c & 1, x);
-                        if (c & 1) {
+                        box_row<T>(box, c % kBoxSteps, x);
+                        if (c % kBoxSteps == kBoxSteps - 1) {
+                            const int c0 = (c - kBoxSteps + 1) * N;      // the box's first column
                             fence_to_tma();
                             __syncwarp();
                             // (row: of lane 0, the box's first; a box that starts outside the result is not stored)
-                            if (lane == 0 && (MODE == kGrad || (c - 1) * 32 < left) && row < most) {
-                                tma_store(dw ? &maps.out2 : &maps.out, box, (int)(col0 + (c - 1) * 32), (int)(dw ? a.v0 + row : row));
+                            if (lane == 0 && (MODE == kGrad || c0 < left) && row < most) {
+                                tma_store(dw ? &maps.out2 : &maps.out, box, (int)(col0 + c0), (int)(dw ? a.v0 + row : row));
                                 tma_store_commit();
                             }
                         }
                     } else if (row < rows) {
-                        store_row32(reinterpret_cast<T *>(a.dx) + (int64_t)a.row_of[row] * a.dx_stride + col0 + c * 32, (int)min((int64_t)32, left - c * 32), x);
+                        store_row(reinterpret_cast<T *>(a.dx) + (int64_t)a.row_of[row] * a.dx_stride + col0 + c * N, (int)min((int64_t)N, left - c * N), x);
                     }
                 }
             }
@@ -897,7 +914,7 @@ cudaError_t launch_product_as(const Maps &maps, const ProductArgs &a, int64_t un
 }
 template <int MODE, typename T>
 cudaError_t launch_product(const Maps &maps, const ProductArgs &a, int64_t units, cudaStream_t st) {
-    if constexpr (MODE == kStats)
+    if constexpr (MODE != kBack)
         if (a.k_blocks > kPass) return launch_product_as<MODE, true, T>(maps, a, units, st);
     return launch_product_as<MODE, false, T>(maps, a, units, st);
 }
