@@ -41,7 +41,7 @@ constexpr int kHalf = 128;                    // rows of either operand that eac
 constexpr int kStages = 6;
 constexpr int kOperand = kHalf * kK * 2;      // bytes
 constexpr int kStage = 2 * kOperand;
-constexpr int kPass = 1024 / kK;              // stages of a logit that one accumulator takes
+constexpr int kPass = 1024 / kK;              // stages that one accumulator takes
 constexpr int kEpilogueWarps = 8;
 constexpr int kProductThreads = 32 * (4 + kEpilogueWarps);
 constexpr int kBox = 32 * 128;                // bytes of what a warp stores at a time: 32 rows of 64 values
@@ -250,10 +250,13 @@ __device__ __forceinline__ float pick(int j, int at, float y, float z) {
 }
 
 // LONG: the depth takes more than one pass.  The tensor cores cut off what an accumulator's last bit cannot hold, product
-// step by product step, which shrinks a logit by some 2^-24 a step; so logits start a new accumulator every kPass stages and
-// add them in registers, rounded to nearest: the losses of 4 096 deep logits are off by 3.4e-7 of themselves so, as those of
-// 1 024 deep ones are, and by over 1e-6 without.  The backward pass takes the same steps, so that its logits are the forward
-// pass's to the last bit: where a target has all the probability, G is exp(z - lse) - 1 = 0 only if lse was made of this z.
+// step by product step, which shrinks a sum of one sign by some 1.5 x 2^-24 of itself per 16 of depth; so every product starts
+// a new accumulator every kPass stages and adds them in registers, rounded to nearest.  Logits: the losses of 4 096 deep ones
+// are off by 3.4e-7 of themselves so, as those of 1 024 deep ones are, and by over 1e-6 without.  The backward pass takes the
+// same steps, so that its logits are the forward pass's to the last bit: where a target has all the probability, G is
+// exp(z - lse) - 1 = 0 only if lse was made of this z.  Gradients, as deep as there are rows or vocabulary entries: dw of
+// 2^21 rows is off by 1.3 % without, by 7e-6 with it (and its rounding).  Passes four and sixteen times as long save up to 1 %
+// of the time and lose 2.5e-5 and 1e-4.
 template <int MODE, bool LONG, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1) __cluster_dims__(2, 1, 1)
 product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ ProductArgs a) {
@@ -401,7 +404,11 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
             float held[LONG ? 128 : 1];
             bool ok = true;
             if constexpr (LONG) {     // all passes but the last are added up in registers
-                for (int p = 0; p + kPass < k_blocks; p += kPass, ++nth) {
+                if (MODE == kBack) {  // (there may be none)
+#pragma unroll
+                    for (int j = 0; j < 128; ++j) held[j] = 0.0f;
+                }
+                for (int p = u.k0; p + kPass < u.k1; p += kPass, ++nth) {
                     const uint32_t acc = nth & 1;
                     ok = __all_sync(0xFFFFFFFFu, wait_for(s, &s.done[acc], (nth >> 1) & 1));   // (the warp stays together)
                     if (!ok) break;
@@ -412,7 +419,7 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
                         tmem_load16(mine + acc * kN + c * 16, r);
                         tmem_load_wait();
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) held[c * 16 + j] = p == 0 ? __uint_as_float(r[j]) : __fadd_rn(held[c * 16 + j], __uint_as_float(r[j]));
+                        for (int j = 0; j < 16; ++j) held[c * 16 + j] = MODE != kBack && p == 0 ? __uint_as_float(r[j]) : __fadd_rn(held[c * 16 + j], __uint_as_float(r[j]));
                     }
                     tc_fence_before();
                     __syncwarp();
@@ -485,14 +492,15 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
                         __syncwarp();
                         if (lane == 0) mbar_arrive_at(freed);
                     }
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        x[j] = __uint_as_float(r[j]);
+                        if constexpr (LONG) x[j] = __fadd_rn(held[c * N + j], x[j]);
+                        if (MODE == kBack && empty) x[j] = 0.0f;
+                    }
                     if constexpr (MODE == kGrad) {
                         const bool here = at >= c * N && at < (c + 1) * N;
                         float y = 0.0f;                                  // the target's logit
-#pragma unroll
-                        for (int j = 0; j < N; ++j) {
-                            x[j] = __uint_as_float(r[j]);
-                            if constexpr (LONG) x[j] = __fadd_rn(held[c * N + j], x[j]);
-                        }
                         if (__any_sync(0xFFFFFFFFu, here)) {
 #pragma unroll
                             for (int j = 0; j < N; ++j) y = pick(c * N + j, at, x[j], y);
@@ -514,8 +522,7 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
 #pragma unroll
                         for (int q = 0; q < N / 4; ++q) {
                             float4 *p = a.partial + partial_at(u.place, rank, half, quarter, c * (N / 4) + q, lane);
-                            float4 y = make_float4(__uint_as_float(r[4 * q]), __uint_as_float(r[4 * q + 1]), __uint_as_float(r[4 * q + 2]), __uint_as_float(r[4 * q + 3]));
-                            if (empty) y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                            float4 y = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
                             if (a.add) {
                                 const float4 z = *p;
                                 y = make_float4(__fadd_rn(z.x, y.x), __fadd_rn(z.y, y.y), __fadd_rn(z.z, y.z), __fadd_rn(z.w, y.w));
@@ -525,7 +532,7 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
                         continue;
                     } else {
 #pragma unroll
-                        for (int j = 0; j < N; ++j) x[j] = empty ? 0.0f : __fmul_rn(__uint_as_float(r[j]), inverse);
+                        for (int j = 0; j < N; ++j) x[j] = __fmul_rn(x[j], inverse);
                     }
                     if (boxes) {
                         if (c % kBoxSteps == 0) {    // the box's memory, once the last store has read it
@@ -914,8 +921,8 @@ cudaError_t launch_product_as(const Maps &maps, const ProductArgs &a, int64_t un
 }
 template <int MODE, typename T>
 cudaError_t launch_product(const Maps &maps, const ProductArgs &a, int64_t units, cudaStream_t st) {
-    if constexpr (MODE != kBack)
-        if (a.k_blocks > kPass) return launch_product_as<MODE, true, T>(maps, a, units, st);
+    const int dw_k = MODE == kBack && a.dw_tiles > 0 ? (a.rows + kK - 1) / kK : 0;
+    if (a.k_blocks > kPass || dw_k > kPass) return launch_product_as<MODE, true, T>(maps, a, units, st);
     return launch_product_as<MODE, false, T>(maps, a, units, st);
 }
 

@@ -11,6 +11,8 @@ pytestmark = pytest.mark.gpu
 
 U32 = 2.0 ** -24
 HALF = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+# An accumulation that is cut into pieces of 1 024: 64 steps, each of which cuts off less than 2 u of it
+PIECE = 64 * 2 * U32
 
 
 @pytest.fixture(scope="module")
@@ -52,3 +54,62 @@ def test_a_certain_target_is_left_alone(ops, dtype, d, far):
     # a float16 dx also rounds to 2^-25 absolutely, in a direction of its own per element
     tol = tol + (2.0 ** -25 * math.sqrt(d) / wt.norm(dim=1) if dtype == torch.float16 else 0.0)
     assert (G.abs() <= tol).all(), (float((G.abs() / tol).max()), float(G.mean()))
+
+
+def one_signed(seed, n, d, v, dtype, sx, sw):
+    """x of either sign and w positive, small logits; every target is entry 0, whose row of w is zero: all terms of dx are
+    positive."""
+    g = gen(seed)
+    sign = torch.randint(0, 2, (n, d), generator=g, device="cuda") * 2 - 1
+    x = ((torch.rand(n, d, generator=g, device="cuda") + 0.5) * sign * sx).to(dtype)
+    w = ((torch.rand(v, d, generator=g, device="cuda") + 0.5) * sw).to(dtype)
+    w[0] = 0
+    return x, w, torch.zeros(n, dtype=torch.int64, device="cuda")
+
+
+def held(p, dtype):
+    """G relative to the largest row weight, as it is held: in float16 2^15 times as large."""
+    scale = 32768.0 if dtype == torch.float16 else 1.0
+    return (p * scale).to(dtype).double() / scale
+
+
+@pytest.mark.parametrize("n,d,v", [(2048, 2048, 131072), (40, 256, 600000)])
+def test_dx_does_not_shrink_with_the_vocabulary(ops, n, d, v):
+    dtype = torch.float16
+    x, w, t = one_signed(1, n, d, v, dtype, 2.0 ** -5, 2.0 ** -9 * math.sqrt(2048 / d))
+    one = torch.ones(1, device="cuda")
+    out = ops.linear_xent(x, w, t)
+    dx = ops.linear_xent_grad(x, w, t, out["lse"], one, out={"dx": torch.empty_like(x)})["dx"].double()
+    xd, wd = x.double(), w.double()
+    # (The target's part falls on a row of zeros.  Both roundings that the operator states are the reference's too: the values
+    # lie so close together that rounding them, near a power of two, has a mean of its own.)
+    p = held(torch.softmax(xd @ wd.T, 1), dtype)
+    want = p @ wd
+    err = float(((dx - want.to(dtype).double()) / want).mean())
+    big = float((xd.abs().sum(1) * wd.amax()).max())
+    # exponentials: three times a logit's error and 2^-20; sums: pieces, added up in float32 (one rounding each)
+    tol = 3 * ((min(d, 1024) / 16 + 16) * 2 * U32 * big + 2.0 ** -20) + PIECE + math.ceil(v / 1024) * U32
+    # values and G that fall on the other side of a rounding's border: no more than if all of them did, six deviations
+    tol += 6 * 2 * HALF[dtype] / math.sqrt(3 * n * d) + 6 * HALF[dtype] / math.sqrt(3 * v)
+    assert abs(err) <= tol, (err, tol)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n,d,v", [(1 << 20, 64, 64), ((1 << 21) - 77, 8, 40)])
+def test_dw_does_not_shrink_with_the_rows(ops, dtype, n, d, v):
+    """The entries that are never a target only collect positive G; x is positive here."""
+    g = gen(n)
+    x = (torch.rand(n, d, generator=g, device="cuda") + 0.5).to(dtype)
+    w = (torch.randn(v, d, generator=g, device="cuda") * (0.1 / d)).to(dtype)
+    t = torch.zeros(n, dtype=torch.int64, device="cuda")
+    one = torch.full((1,), 64.0 / n, device="cuda")
+    out = ops.linear_xent(x, w, t)
+    dw = ops.linear_xent_grad(x, w, t, out["lse"], one, out={"dw": torch.empty_like(w)})["dw"][1:].double()
+    xd, wd = x.double(), w.double()
+    p = held(torch.softmax(xd @ wd.T, 1), dtype)
+    want = (p.T @ xd * float(one))[1:]
+    err = float(((dw - want.to(dtype).double()) / want).mean())
+    big = float((xd @ wd.abs().T).max())
+    tol = 3 * ((d / 16 + 16) * 2 * U32 * big + 2.0 ** -20) + PIECE + math.ceil(n / 1024) * U32
+    tol += 6 * HALF[dtype] / math.sqrt(3 * d * (v - 1)) + 6 * HALF[dtype] / math.sqrt(3 * n)
+    assert abs(err) <= tol, (err, tol)
