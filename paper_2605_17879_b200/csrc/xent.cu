@@ -645,7 +645,7 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a, const
             const bool bad = t[j] != a.ignore && (t[j] < 0 || t[j] >= a.vocab);
             if (t[j] != a.ignore && !bad) {
                 in |= 1u << j;
-                top = fmaxf(top, fabsf(g[j]));
+                if (fabsf(g[j]) < INFINITY) top = fmaxf(top, fabsf(g[j]));      // (others spoil their own rows alone)
             } else if (writes && first + j < a.rows) {
                 if (bad && a.status) atomicOr(a.status, kStatIndex);
                 if (a.loss) {
@@ -697,7 +697,7 @@ __global__ void __launch_bounds__(1024) xent_rows_kernel(const RowsArgs a, const
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int w = 0; w < 32; ++w) top = fmaxf(top, s_top[w]);
-        const bool plain = !(top >= 1e-30f && top < INFINITY);     // (the products could leave float32's range)
+        const bool plain = !(top >= 1e-30f);     // (the products could leave float32's range)
         a.head->count = before;
         a.head->whole = before == a.rows;
         a.head->unit = plain ? 1.0f : top;
