@@ -63,8 +63,9 @@ def gather(mine: torch.Tensor) -> torch.Tensor:
     """Every rank's tensor (all of one shape), rank by rank along a new first dimension, on every rank."""
     if not dist.is_initialized():
         return mine.unsqueeze(0)
+    mine = mine.contiguous()
     parts = [torch.empty_like(mine) for _ in range(dist.get_world_size())]
-    dist.all_gather(parts, mine.contiguous())
+    dist.all_gather(parts, mine)
     return torch.stack(parts)
 
 

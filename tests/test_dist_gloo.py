@@ -79,3 +79,18 @@ def test_gather_of_a_single_process():
     import torch
     from paper_2605_17879_b200 import dist as gd
     assert gd.gather(torch.ones(3, 4)).shape == (1, 3, 4)
+
+
+def test_gather_keeps_the_order_of_a_transposed_tensor(monkeypatch):
+    """A collective moves memory as it lies, so what receives must lie like what is sent."""
+    import torch
+    from paper_2605_17879_b200 import dist as gd
+
+    def all_gather(parts, mine):
+        for p in parts:
+            torch.as_strided(p, (p.numel(),), (1,)).copy_(torch.as_strided(mine, (mine.numel(),), (1,)))
+    monkeypatch.setattr(gd.dist, "is_initialized", lambda: True)
+    monkeypatch.setattr(gd.dist, "get_world_size", lambda: 2)
+    monkeypatch.setattr(gd.dist, "all_gather", all_gather)
+    for mine in (torch.arange(12.0).view(4, 3).t(), torch.arange(12.0).view(4, 3)[:, :2], torch.arange(6.0)):
+        assert torch.equal(gd.gather(mine), torch.stack([mine, mine]))
