@@ -9,7 +9,8 @@ of the current ones with the same table (tied weights).  A step is
 with the library's own operators (operators.py).  Its parts load what a job's step loads and a product or a copy alone does
 not: irregular reads of the table (embed), the tensor cores under the power limit (loss and gradients), a sort and sums over
 frequent tokens (embed_grad), and a stream over all of parameters and states (AdamW).  Every part is deterministic, so GPUs
-that start from the same seed must report the same losses, bit for bit; one that does not computes wrong results.
+that start from the same seed must report the same losses, bit for bit; one that does not computes wrong results and fails.
+The command prints the verdict as one line of JSON and returns 1 where results disagree.
 
     python -m paper_2605_17879_b200.sweep_run                                         one GPU
     torchrun --standalone --local-addr 127.0.0.1 --nproc-per-node 8 -m paper_2605_17879_b200.sweep_run     a node
@@ -20,7 +21,8 @@ import argparse
 import json
 import math
 import sys
-from typing import Dict, Optional
+from collections import Counter
+from typing import Dict, List, Optional
 
 import torch
 
@@ -114,6 +116,27 @@ def qualify(rows: torch.Tensor, nodes: int, gpus_per_node: int, **kw):
     return guard.sweep_qualify(rows.contiguous(), nodes, gpus_per_node, dir=DIR, **kw)
 
 
+def agreement(losses: torch.Tensor) -> List[Optional[bool]]:
+    """Which GPUs computed what most of them did: losses [gpus, reps], compared whole and bit for bit.  True and False where a
+    strict majority agrees, None for all where there is none."""
+    rows = [tuple(r) for r in losses.contiguous().view(torch.int32).tolist()]
+    common, count = Counter(rows).most_common(1)[0] if rows else ((), 0)
+    return [r == common for r in rows] if 2 * count > len(rows) else [None] * len(rows)
+
+
+def verdict(rows: torch.Tensor, losses: torch.Tensor, nodes: int, gpus_per_node: int, judge=qualify) -> Dict[str, object]:
+    """What the fleet's results say: rows [gpus, reps, 4], losses [gpus, reps].  A GPU that computed other losses than the
+    majority fails, and its node with it."""
+    gpus, reps = losses.shape
+    out = judge(rows, nodes, gpus_per_node)
+    same = agreement(losses)
+    gpu_pass = [int(bool(ok) and equal is not False) for ok, equal in zip(out["gpu_pass"].tolist(), same)]
+    return {"metrics": METRICS, "gpus": gpus, "reps": reps,
+            "medians": [dict(zip(METRICS, [round(float(x), 3) for x in row])) for row in out["gpu_med"].cpu()], "gpu_pass": gpu_pass,
+            "node_pass": [min(gpu_pass[n:n + gpus_per_node]) for n in range(0, gpus, gpus_per_node)], "fail_mask": out["fail_mask"].tolist(),
+            "same_results": same, "last_loss": float(losses[0, -1])}
+
+
 def main(argv: Optional[list] = None) -> int:
     ap = argparse.ArgumentParser(description="Runs the sweep's load on every rank's GPU and qualifies the GPUs against one another.")
     ap.add_argument("--reps", type=int, default=20)
@@ -134,16 +157,14 @@ def main(argv: Optional[list] = None) -> int:
     gd.barrier()
     got = load.measure(args.reps)
     S, losses = gd.gather(got["rows"]), gd.gather(got["loss"])
+    code = 0
     if rank == 0:
-        out = qualify(S, world // per_node, per_node)
-        common = losses.mode(0).values                              # what most GPUs computed
-        print(json.dumps({
-            "metrics": METRICS, "gpus": world, "reps": args.reps,
-            "medians": [dict(zip(METRICS, [round(float(x), 3) for x in row])) for row in out["gpu_med"].cpu()],
-            "gpu_pass": out["gpu_pass"].tolist(), "node_pass": out["node_pass"].tolist(), "fail_mask": out["fail_mask"].tolist(),
-            "same_results": [bool(torch.equal(row, common)) for row in losses], "last_loss": float(losses[0, -1])}), flush=True)
+        report = verdict(S, losses, world // per_node, per_node)
+        print(json.dumps(report), flush=True)
+        code = int(not all(report["same_results"]))
+    gd.barrier()                    # (a launcher ends the other ranks when one returns an error)
     gd.finish()
-    return 0
+    return code
 
 
 if __name__ == "__main__":

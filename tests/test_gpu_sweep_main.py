@@ -1,0 +1,14 @@
+"""The node sweep's command on one GPU, from its arguments to its line of JSON."""
+import json
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def test_main_reports_one_gpu(capsys):
+    from paper_2605_17879_b200 import sweep_run
+    assert sweep_run.main(["--reps", "4", "--rows", "300", "--width", "64", "--vocab", "500"]) == 0
+    got = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
+    assert got["gpus"] == 1 and got["reps"] == 4 and got["gpu_pass"] == [1] and got["node_pass"] == [1] and got["same_results"] == [True]
+    assert all(x > 0 for x in got["medians"][0].values()) and got["last_loss"] > 0
