@@ -10,7 +10,8 @@ with the library's own operators (operators.py).  Its parts load what a job's st
 not: irregular reads of the table (embed), the tensor cores under the power limit (loss and gradients), a sort and sums over
 frequent tokens (embed_grad), and a stream over all of parameters and states (AdamW).  Every part is deterministic, so GPUs
 that start from the same seed must report the same losses, bit for bit; one that does not computes wrong results and fails.
-The command prints the verdict as one line of JSON and returns 1 where results disagree.
+So does one whose load raises an error; the others are judged without it.  The command prints the verdict as one line of JSON
+and returns 1 where a load failed or results disagree.
 
     python -m paper_2605_17879_b200.sweep_run                                         one GPU
     torchrun --standalone --local-addr 127.0.0.1 --nproc-per-node 8 -m paper_2605_17879_b200.sweep_run     a node
@@ -22,7 +23,7 @@ import json
 import math
 import sys
 from collections import Counter
-from typing import Dict, List, Optional
+from typing import Dict, List, Optional, Sequence, Tuple
 
 import torch
 
@@ -124,17 +125,53 @@ def agreement(losses: torch.Tensor) -> List[Optional[bool]]:
     return [r == common for r in rows] if 2 * count > len(rows) else [None] * len(rows)
 
 
-def verdict(rows: torch.Tensor, losses: torch.Tensor, nodes: int, gpus_per_node: int, judge=qualify) -> Dict[str, object]:
-    """What the fleet's results say: rows [gpus, reps, 4], losses [gpus, reps].  A GPU that computed other losses than the
-    majority fails, and its node with it."""
+def verdict(rows: torch.Tensor, losses: torch.Tensor, failed: Sequence[bool], gpus_per_node: int, judge=qualify) -> Dict[str, object]:
+    """What the fleet's results say.  rows [gpus, reps, 4], losses [gpus, reps], failed: GPUs whose load raised an error, whose
+    results say nothing.  Those fail; the others are qualified against one another, and fail too where they computed other
+    losses than the majority.  A node passes when all its GPUs pass."""
     gpus, reps = losses.shape
-    out = judge(rows, nodes, gpus_per_node)
-    same = agreement(losses)
-    gpu_pass = [int(bool(ok) and equal is not False) for ok, equal in zip(out["gpu_pass"].tolist(), same)]
-    return {"metrics": METRICS, "gpus": gpus, "reps": reps,
-            "medians": [dict(zip(METRICS, [round(float(x), 3) for x in row])) for row in out["gpu_med"].cpu()], "gpu_pass": gpu_pass,
-            "node_pass": [min(gpu_pass[n:n + gpus_per_node]) for n in range(0, gpus, gpus_per_node)], "fail_mask": out["fail_mask"].tolist(),
-            "same_results": same, "last_loss": float(losses[0, -1])}
+    good = [g for g in range(gpus) if not failed[g]]
+    medians, fail_mask, same = [None] * gpus, [None] * gpus, [None] * gpus
+    gpu_pass = [0] * gpus
+    if good:
+        out = judge(rows[good], len(good), 1)
+        equal = agreement(losses[good])
+        for k, g in enumerate(good):
+            medians[g] = dict(zip(METRICS, [round(float(x), 3) for x in out["gpu_med"][k]]))
+            fail_mask[g], same[g] = int(out["fail_mask"][k]), equal[k]
+            gpu_pass[g] = int(bool(out["gpu_pass"][k]) and equal[k] is not False)
+    return {"metrics": METRICS, "gpus": gpus, "reps": reps, "medians": medians, "gpu_pass": gpu_pass,
+            "node_pass": [min(gpu_pass[n:n + gpus_per_node]) for n in range(0, gpus, gpus_per_node)], "fail_mask": fail_mask,
+            "same_results": same, "load_failed": [bool(f) for f in failed], "last_loss": float(losses[good[0], -1]) if good else None}
+
+
+def sweep(make, reps: int, gpus_per_node: int, judge=qualify) -> Tuple[Optional[Dict[str, object]], int]:
+    """Runs the load make() on this rank and collects every rank's results on the host, where a GPU that failed its load can
+    still report.  Returns the verdict on the first rank whose load ran (None on the others), and 1 where this rank's load
+    failed or the results that were collected disagree."""
+    rank, _, _ = gd.env_world()
+    rows, loss, load = torch.full((reps, len(METRICS)), math.nan), torch.full((reps,), math.nan), None
+    error = None
+    try:
+        load = make()
+    except (guard.GuardError, RuntimeError) as e:
+        error = e
+    gd.barrier()                    # all of them start together
+    try:
+        if load is not None:
+            got = load.measure(reps)
+            rows, loss = got["rows"].cpu(), got["loss"].cpu()
+    except (guard.GuardError, RuntimeError) as e:
+        error = e
+    if error is not None:
+        print("rank %d: the load failed: %s" % (rank, error), file=sys.stderr, flush=True)
+    failed = gd.gather(torch.tensor([error is not None])).flatten().tolist()
+    S, losses = gd.gather(rows), gd.gather(loss)
+    if rank != (failed.index(False) if False in failed else 0):
+        return None, int(error is not None)
+    report = verdict(S, losses, failed, gpus_per_node, judge)
+    agree = all(report["same_results"][g] is True for g in range(len(failed)) if not failed[g])
+    return report, int(error is not None or not agree)
 
 
 def main(argv: Optional[list] = None) -> int:
@@ -148,20 +185,19 @@ def main(argv: Optional[list] = None) -> int:
     args = ap.parse_args(argv)
     if not torch.cuda.is_available():
         raise SystemExit("sweep_run needs a CUDA device (there is no CPU fallback)")
-    rank, local_rank, world = gd.init("nccl")
+    if args.reps < 1:
+        raise SystemExit("--reps must be at least 1")
+    # (the ranks exchange rows of results only, and those on the host)
+    rank, local_rank, world = gd.init("gloo")
     per_node = args.gpus_per_node or world
     if world % per_node:
         raise SystemExit("the number of ranks must be a multiple of --gpus-per-node")
-    torch.cuda.set_device(local_rank)
-    load = SweepStep(rows=args.rows, width=args.width, vocab=args.vocab, state_bits=args.state_bits, device=torch.device("cuda", local_rank))
-    gd.barrier()
-    got = load.measure(args.reps)
-    S, losses = gd.gather(got["rows"]), gd.gather(got["loss"])
-    code = 0
-    if rank == 0:
-        report = verdict(S, losses, world // per_node, per_node)
+    device = torch.device("cuda", local_rank)
+    torch.cuda.set_device(device)
+    report, code = sweep(lambda: SweepStep(rows=args.rows, width=args.width, vocab=args.vocab, state_bits=args.state_bits, device=device),
+                         args.reps, per_node, lambda S, nodes, per: {k: v.cpu() for k, v in qualify(S.to(device), nodes, per).items()})
+    if report is not None:
         print(json.dumps(report), flush=True)
-        code = int(not all(report["same_results"]))
     gd.barrier()                    # (a launcher ends the other ranks when one returns an error)
     gd.finish()
     return code
