@@ -440,6 +440,12 @@ int guard_linear_xent_grad(const void *d_x, int64_t x_stride, const void *d_w, i
                            const float *d_lse, const float *d_grad_loss, int grad_stride, void *d_dx, void *d_dw,
                            void *d_workspace, size_t workspace_bytes, uint32_t *d_status, void *stream);
 
+/* Test hook: limit, in clock cycles, of the waits in guard_linear_xent and guard_linear_xent_grad from now on (0 restores
+ * the default of about a second).  With a short limit waits run out while copies and products are in flight; the kernels
+ * then let those land, set GUARD_STATUS_TIMEOUT and return, and later calls work.  Exists so that this path can be
+ * exercised. */
+int guard_debug_set_operator_wait_limit(long long cycles);
+
 /*
  * AdamW over many tensors in one launch.  Step t of a parameter p with gradient g (all in float32):
  *   g' = grad_scale * g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2;

@@ -23,6 +23,16 @@ __device__ __forceinline__ uint32_t in_first(const void *p) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(p)));
     return r;
 }
+// A word of shared memory, at the same place in the pair's CTA of that rank (the pair's next meeting orders it).
+__device__ __forceinline__ void store_in_pair(const void *p, uint32_t rank, uint32_t value) {
+    asm volatile("{\n\t.reg .b32 r;\n\tmapa.shared::cluster.u32 r, %0, %1;\n\tst.relaxed.cluster.shared::cluster.u32 [r], %2;\n\t}" ::"r"(smem_u32(p)),
+                 "r"(rank), "r"(value)
+                 : "memory");
+}
+// Counts bytes on a barrier of this CTA as copied which no copy will bring.
+__device__ __forceinline__ void mbar_complete_tx(uint64_t *bar, uint32_t bytes) {
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
 // An arrival that orders no memory: for TMEM reads, which tcgen05.wait::ld and the fence before it have completed.  (The
 // releasing form waits for the thread's global stores to reach the whole GPU.)
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_address) {

@@ -145,6 +145,13 @@ size_t guard_linear_xent_workspace_bytes(int64_t rows, int64_t width, int64_t vo
     return xent_workspace(rows, width, vocab, grads != 0);
 }
 
+static std::atomic<long long> g_wait_limit{0};
+
+int guard_debug_set_operator_wait_limit(long long cycles) {
+    if (cycles < 0) return call_error(GUARD_ERR_ARG, "cycles must not be negative");
+    g_wait_limit.store(cycles, std::memory_order_relaxed);
+    return GUARD_OK;
+}
 // The checks that both directions share; 0 or an error.
 static int xent_check(const XentArgs &a, size_t need, size_t given, const void *out0, size_t n0, const void *out1, size_t n1) {
     if ((a.dtype != GUARD_BF16 && a.dtype != GUARD_F16) || (a.target_bits != 32 && a.target_bits != 64))
@@ -185,6 +192,7 @@ int guard_linear_xent(const void *d_x, int64_t x_stride, const void *d_w, int64_
     a.lse_out = d_lse;
     a.workspace = d_workspace;
     a.status = d_status;
+    a.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
     if (!d_loss || !d_lse || !on(d_loss, 4) || !on(d_lse, 4)) return call_error(GUARD_ERR_ARG, "d_loss and d_lse must be non-NULL and aligned to their elements");
     const int rc = xent_check(a, guard_linear_xent_workspace_bytes(rows, width, vocab, 0), workspace_bytes, d_loss, (size_t)rows * 4, d_lse, (size_t)rows * 4);
     if (rc != GUARD_OK) return rc;
@@ -224,6 +232,7 @@ int guard_linear_xent_grad(const void *d_x, int64_t x_stride, const void *d_w, i
     a.dw = d_dw;
     a.workspace = d_workspace;
     a.status = d_status;
+    a.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
     if (!d_lse || !d_grad_loss || !on(d_lse, 4) || !on(d_grad_loss, 4)) return call_error(GUARD_ERR_ARG, "d_lse and d_grad_loss must be non-NULL and aligned to their elements");
     const int rc = xent_check(a, guard_linear_xent_workspace_bytes(rows, width, vocab, 1), workspace_bytes, d_dx, (size_t)rows * width * 2, d_dw, (size_t)vocab * width * 2);
     if (rc != GUARD_OK) return rc;

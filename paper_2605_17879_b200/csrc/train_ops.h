@@ -123,6 +123,7 @@ struct XentArgs {
     int64_t grad_stride;     // 0 or 1
     void *dx, *dw;           // or NULL
     void *workspace;
+    long long wait_limit;    // cycles, of each wait between the warps of the products (0: about a second)
     uint32_t *status;
 };
 size_t xent_workspace(int64_t rows, int64_t width, int64_t vocab, bool grads);

@@ -80,6 +80,7 @@ struct ProductArgs {
     float4 *partial;       // or NULL: partial sums of dx by tile and split, as threads hold them (see partial_at)
     int max_units, max_splits;        // places in it, and splits that the depth allows
     int add;               // add to partial
+    long long wait_limit;  // cycles, or 0
     uint32_t *status;
 };
 
@@ -94,20 +95,40 @@ __device__ __forceinline__ float finite_or_zero(float m) { return fabsf(m) == IN
 struct alignas(8) ProductShared {
     uint64_t full[kStages], empty[kStages], done[2], free_[2], drain;
     uint32_t tmem;
-    uint32_t abort;
+    uint32_t abort;        // a wait ran out in this CTA; in either of the pair, once they have met
+    uint32_t issued[2];    // in the first CTA: stages that each CTA of the pair has issued copies for
 };
 
-// Bounded wait; false when the time ran out here or in another warp.
-__device__ __forceinline__ bool wait_for(ProductShared &s, uint64_t *bar, uint32_t parity) {
+// Bounded wait; false when the time ran out here or in another warp.  POLL: with a test's short limit (a waiting instruction
+// may sleep beyond it); an instance of its own, since a limit that is looked up costs the forward pass 2 %.
+template <bool POLL>
+__device__ __forceinline__ bool wait_for(ProductShared &s, uint64_t *bar, uint32_t parity, long long limit) {
     const long long t0 = clock64();
-    while (!mbar_try_wait(bar, parity)) {
+    while (!(POLL ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity))) {
         if (*(volatile uint32_t *)&s.abort) return false;
-        if (clock64() - t0 > kWaitLimitCycles) {
+        if (clock64() - t0 > (POLL ? limit : kWaitLimitCycles)) {
             *(volatile uint32_t *)&s.abort = 1;
             return false;
         }
     }
     return true;
+}
+// What a wait that ran out leaves in flight, once nobody of the pair issues any more: copies into the memory of either CTA,
+// counted on the first one's barriers, and products.  Waits for them, a second at most.
+__device__ __forceinline__ void land_copies(ProductShared &s) {      // one thread of the first CTA
+    const long long t0 = clock64();
+    const uint32_t armed = s.issued[0], other = s.issued[1], most = max(armed, other);
+    for (uint32_t i = most > kStages ? most - kStages : 0; i < most; ++i) {
+        uint64_t *bar = &s.full[i % kStages];
+        // a barrier is armed by the first CTA, for the bytes of both
+        if (i >= armed) mbar_arrive_expect_tx(bar, kStage);
+        else if (i >= other) mbar_complete_tx(bar, kStage);
+        while (!mbar_try_wait(bar, (i / kStages) & 1) && clock64() - t0 < kWaitLimitCycles) {}
+    }
+}
+__device__ __forceinline__ void land_products(ProductShared &s) {
+    const long long t0 = clock64();
+    while (!mbar_try_wait(&s.drain, 0) && clock64() - t0 < kWaitLimitCycles) {}
 }
 
 // Parts into which the depth of dx is split: as many as keep every pair of CTAs busy and have a place.
@@ -257,7 +278,7 @@ __device__ __forceinline__ float pick(int j, int at, float y, float z) {
 // exp(z - lse) - 1 = 0 only if lse was made of this z.  Gradients, as deep as there are rows or vocabulary entries: dw of
 // 2^21 rows is off by 1.3 % without, by 7e-6 with it (and its rounding).  Passes four and sixteen times as long save up to 1 %
 // of the time and lose 2.5e-5 and 1e-4.
-template <int MODE, bool LONG, typename T>
+template <int MODE, bool LONG, bool POLL, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1) __cluster_dims__(2, 1, 1)
 product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ ProductArgs a) {
     extern __shared__ uint8_t raw[];
@@ -271,7 +292,7 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
     const bool whole = a.head ? a.head->whole != 0 : true;
     Work work;
     work.begin<MODE>(a, rows);
-    const int k_blocks = a.k_blocks, pass = LONG ? kPass : INT32_MAX / 2;      // stages an accumulator takes
+    const int pass = LONG ? kPass : INT32_MAX / 2;      // stages an accumulator takes
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
@@ -284,6 +305,7 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
         }
         mbar_init(&s.drain, 1);
         s.abort = 0;
+        s.issued[0] = s.issued[1] = 0;
     }
     if (warp == 2) tmem_alloc(&s.tmem, 512);
     tc_fence_before();
@@ -309,7 +331,7 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
             const int m0 = u.m * kM + rank * kHalf, n0 = u.n * kN + rank * kHalf;
             for (int k = u.k0; k < u.k1; ++k, ++it) {
                 const int st = it % kStages;
-                if (!(ok = wait_for(s, &s.empty[st], ((it / kStages) & 1) ^ 1))) break;
+                if (!(ok = wait_for<POLL>(s, &s.empty[st], ((it / kStages) & 1) ^ 1, a.wait_limit))) break;
                 uint8_t *sa = tiles + st * kStage, *sb = sa + kOperand;
                 const uint32_t full = in_first(&s.full[st]);
                 if (rank == 0) mbar_arrive_expect_tx(&s.full[st], 2 * kStage);      // of both CTAs
@@ -326,12 +348,7 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
                 }
             }
         }
-        if (rank == 0 && *(volatile uint32_t *)&s.abort) {       // given up: let the copies in flight land before the memory is anyone else's
-            for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) {
-                const long long t0 = clock64();
-                while (!mbar_try_wait(&s.full[i % kStages], (i / kStages) & 1) && clock64() - t0 < kWaitLimitCycles) {}
-            }
-        }
+        store_in_pair(&s.issued[rank], 0, it);
     } else if (warp == 1 && lane == 0 && rank == 0) {
         // ---- products
         constexpr uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
@@ -349,11 +366,11 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
             for (int p0 = k0; ok; p0 += pass, ++nth) {          // (once even where there is no depth)
                 const uint32_t acc = nth & 1;
                 const int p1 = min(k1, LONG ? p0 + pass : k1);
-                if (!(ok = wait_for(s, &s.free_[acc], ((nth >> 1) & 1) ^ 1))) break;
+                if (!(ok = wait_for<POLL>(s, &s.free_[acc], ((nth >> 1) & 1) ^ 1, a.wait_limit))) break;
                 tc_fence_after();
                 for (int k = p0; k < p1; ++k, ++it) {
                     const int st = it % kStages;
-                    if (!(ok = wait_for(s, &s.full[st], (it / kStages) & 1))) break;
+                    if (!(ok = wait_for<POLL>(s, &s.full[st], (it / kStages) & 1, a.wait_limit))) break;
                     tc_fence_after();
                     const uint8_t *sa = tiles + st * kStage, *sb = sa + kOperand;
 #pragma unroll
@@ -370,11 +387,6 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
                     break;
                 }
             }
-        }
-        if (*(volatile uint32_t *)&s.abort) {
-            tc_commit(&s.drain);
-            const long long t0 = clock64();
-            while (!mbar_try_wait(&s.drain, 0) && clock64() - t0 < kWaitLimitCycles) {}
         }
     } else if (warp >= 4) {
         // ---- what becomes of an accumulator: a thread has a row, and half of its columns
@@ -410,7 +422,7 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
                 }
                 for (int p = u.k0; p + kPass < u.k1; p += kPass, ++nth) {
                     const uint32_t acc = nth & 1;
-                    ok = __all_sync(0xFFFFFFFFu, wait_for(s, &s.done[acc], (nth >> 1) & 1));   // (the warp stays together)
+                    ok = __all_sync(0xFFFFFFFFu, wait_for<POLL>(s, &s.done[acc], (nth >> 1) & 1, a.wait_limit));   // (the warp stays together)
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll
@@ -428,7 +440,7 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
                 if (!ok) break;
             }
             const uint32_t acc = nth & 1;
-            if (!__all_sync(0xFFFFFFFFu, wait_for(s, &s.done[acc], (nth >> 1) & 1))) break;
+            if (!__all_sync(0xFFFFFFFFu, wait_for<POLL>(s, &s.done[acc], (nth >> 1) & 1, a.wait_limit))) break;
             ++nth;
             tc_fence_after();
             const uint32_t from = mine + acc * kN, freed = acc ? free1 : free0;
@@ -559,10 +571,21 @@ product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Produc
         if (MODE != kStats && lane == 0) tma_store_wait();
     }
     tc_fence_before();
+    if (*(volatile uint32_t *)&s.abort) store_in_pair(&s.abort, rank ^ 1, 1);      // (whoever set it comes here after that)
     __syncwarp();
     cluster_sync();              // the pair's memory and barriers are used by both until here
     tc_fence_after();
-    if (threadIdx.x == 0 && s.abort && a.status) atomicOr(a.status, kStatTimeout);
+    if (s.abort) {
+        if (warp == 0 && lane == 0 && rank == 0) land_copies(s);
+        if (warp == 1 && lane == 0) {
+            if (rank == 0) tc_commit(&s.drain);      // (of this thread's products)
+            land_products(s);
+        }
+        if (threadIdx.x == 0 && a.status) atomicOr(a.status, kStatTimeout);
+        __syncwarp();
+        cluster_sync();
+        tc_fence_after();
+    }
     if (warp == 2) tmem_free(tmem, 512);
 }
 
@@ -911,19 +934,20 @@ XentLayout layout(int64_t rows, int64_t width, int64_t vocab, bool grads) {
     return L;
 }
 
-template <int MODE, bool LONG, typename T>
+template <int MODE, bool LONG, bool POLL, typename T>
 cudaError_t launch_product_as(const Maps &maps, const ProductArgs &a, int64_t units, cudaStream_t st) {
     static SmemAttribute wide;
-    const cudaError_t e = wide.set((const void *)product_kernel<MODE, LONG, T>, kProductSmem);
+    const cudaError_t e = wide.set((const void *)product_kernel<MODE, LONG, POLL, T>, kProductSmem);
     if (e != cudaSuccess) return e;
     const int64_t pairs = sm_count() / 2;
-    return launch_after_smem(product_kernel<MODE, LONG, T>, dim3((unsigned)(2 * (units < pairs ? units : pairs))), dim3(kProductThreads), kProductSmem, st, maps, a);
+    return launch_after_smem(product_kernel<MODE, LONG, POLL, T>, dim3((unsigned)(2 * (units < pairs ? units : pairs))), dim3(kProductThreads), kProductSmem, st, maps, a);
 }
 template <int MODE, typename T>
 cudaError_t launch_product(const Maps &maps, const ProductArgs &a, int64_t units, cudaStream_t st) {
     const int dw_k = MODE == kBack && a.dw_tiles > 0 ? (a.rows + kK - 1) / kK : 0;
-    if (a.k_blocks > kPass || dw_k > kPass) return launch_product_as<MODE, true, T>(maps, a, units, st);
-    return launch_product_as<MODE, false, T>(maps, a, units, st);
+    const bool deep = a.k_blocks > kPass || dw_k > kPass;
+    if (a.wait_limit > 0) return deep ? launch_product_as<MODE, true, true, T>(maps, a, units, st) : launch_product_as<MODE, false, true, T>(maps, a, units, st);
+    return deep ? launch_product_as<MODE, true, false, T>(maps, a, units, st) : launch_product_as<MODE, false, false, T>(maps, a, units, st);
 }
 
 // Row tiles that share a column tile: as many as fit in about a third of the second-level cache.
@@ -1011,6 +1035,7 @@ cudaError_t forward(const XentArgs &x, cudaStream_t st) {
     a.n_parts = L.n_parts;
     a.picked = (float *)(ws + L.picked);
     a.status = x.status;
+    a.wait_limit = x.wait_limit;
     e = launch_product<kStats, T>(maps, a, (int64_t)a.m_tiles * a.n_tiles, st);
     if (e != cudaSuccess) return e;
     CombineArgs c{};
@@ -1060,6 +1085,7 @@ cudaError_t backward(const XentArgs &x, cudaStream_t st) {
     a.grad = (const float *)(ws + L.grad);
     a.row_of = (const int32_t *)(ws + L.row_of);
     a.status = x.status;
+    a.wait_limit = x.wait_limit;
     const int row_tiles = (int)(L.padded / kM), width_tiles = (int)((x.width + kN - 1) / kN);
     for (int64_t p = 0; p < pieces; ++p) {
         a.v0 = p * L.piece;

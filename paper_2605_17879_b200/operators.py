@@ -46,6 +46,7 @@ def lib():
                 ("guard_linear_xent_workspace_bytes", z, [i64, i64, i64, i]),
                 ("guard_linear_xent", i, [vp, i64, vp, i64, i64, i64, i64, i, vp, i, i64, vp, vp, vp, z, vp, vp]),
                 ("guard_linear_xent_grad", i, [vp, i64, vp, i64, i64, i64, i64, i, vp, i, i64, vp, vp, i, vp, vp, vp, z, vp, vp]),
+                ("guard_debug_set_operator_wait_limit", i, [C.c_longlong]),
                 ("guard_adamw_blocks", i64, [tp, i]),
                 ("guard_adamw_workspace_bytes", z, [tp, i]),
                 ("guard_adamw_create", i, [C.POINTER(vp), tp, i, i, i, i, d, d, d, vp, vp, vp, vp, i64, C.c_uint32, vp, z, vp]),
@@ -129,6 +130,11 @@ def sync_status(device=None) -> None:
             if bits & STATUS_TIMEOUT:
                 raise GuardError(-5, "a bounded wait of an operator ran out: its results are unspecified")
             raise GuardError(-1, "a token or target lies outside its table")
+
+
+def debug_set_wait_limit(cycles: int) -> None:
+    """Test hook: limit in clock cycles of the waits inside the cross entropy's kernels (0: the default)."""
+    _check(lib().guard_debug_set_operator_wait_limit(int(cycles)))
 
 
 def embed(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.0,

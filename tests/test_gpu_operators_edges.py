@@ -35,3 +35,44 @@ def test_a_weight_that_is_not_finite_reaches_its_row_of_dx_alone(ops, dtype, wei
     assert not got[17].isfinite().any()
     # all of them: nothing to be relative to
     assert not ops.linear_xent_grad(x, w, t, out["lse"], torch.full((1,), weight, device="cuda"))["dx"].isfinite().any()
+
+
+@pytest.mark.parametrize("limit", [1, 300, 3000, 10000, 30000, 90000])
+@pytest.mark.parametrize("n,d,v", [(300, 256, 3000), (600, 2048, 20000), (60, 512, 8192)])
+def test_a_wait_that_runs_out_is_reported_and_later_calls_work(ops, n, d, v, limit):
+    """With a limit of some clock cycles waits inside the products run out, at the first stage or in the middle of the work,
+    while copies and products are in flight.  The kernels let those land and return; a call that reports nothing is right."""
+    g = gen(n)
+    x = torch.randn(n, d, generator=g, device="cuda").bfloat16()
+    w = (torch.randn(v, d, generator=g, device="cuda") * (2 / d ** 0.5)).bfloat16()
+    t = torch.randint(0, v, (n,), generator=g, device="cuda")
+    one = torch.full((1,), 1.0 / n, device="cuda")
+    want = ops.linear_xent(x, w, t)
+    back = ops.linear_xent_grad(x, w, t, want["lse"], one)
+    ops.sync_status()
+
+    def status():
+        return torch.zeros(1, dtype=torch.uint32, device="cuda")
+    ran_out = 0
+    for _ in range(5):
+        out = {"loss": torch.empty(n, device="cuda"), "lse": torch.empty(n, device="cuda"), "status": status()}
+        grads = {"dx": torch.empty_like(x), "dw": torch.empty_like(w), "status": status()}
+        ops.debug_set_wait_limit(limit)
+        try:
+            ops.linear_xent(x, w, t, out=out)
+            ops.linear_xent_grad(x, w, t, want["lse"], one, out=grads)
+        finally:
+            ops.debug_set_wait_limit(0)
+        torch.cuda.synchronize()
+        for got, ref in ((out, want), (grads, back)):
+            bits = int(got["status"].item())
+            assert bits in (0, ops.STATUS_TIMEOUT)
+            ran_out += bits != 0
+            if not bits:
+                assert all(torch.equal(got[k], ref[k]) for k in ref)
+        again = ops.linear_xent(x, w, t)
+        again_back = ops.linear_xent_grad(x, w, t, again["lse"], one)
+        ops.sync_status()
+        assert torch.equal(again["loss"], want["loss"]) and torch.equal(again_back["dx"], back["dx"]) and torch.equal(again_back["dw"], back["dw"])
+    if limit == 1:
+        assert ran_out == 10

@@ -118,3 +118,11 @@ def test_binding_refusals(L):
     with pytest.raises(ValueError):
         ops.linear_xent_grad(x, x, ids, x, x)
     assert ops.AdamW.state_blocks([torch.zeros(0), torch.zeros(257)]) == 2
+
+
+def test_wait_limit_refusals(L):
+    from paper_2605_17879_b200 import operators as ops
+    assert L.guard_debug_set_operator_wait_limit(-1) == -1 and text(L)
+    with pytest.raises(ops.GuardError):
+        ops.debug_set_wait_limit(-5)
+    ops.debug_set_wait_limit(0)
