@@ -52,6 +52,12 @@ int launched(cudaError_t e, const char *what) {
 bool good_matrix(int64_t rows, int64_t width, int64_t stride) {
     return rows >= 0 && width >= 1 && width <= (1 << 24) && stride >= width && stride < (1LL << 40) && rows < (1LL << 60) / stride;
 }
+// The status word and other scalars that kernels access.
+bool good_word(const void *p, const char *name) {
+    if (on(p, 4)) return true;
+    call_error(GUARD_ERR_ARG, "%s is not aligned to its four bytes", name);
+    return false;
+}
 bool overlap(const void *a, size_t na, const void *b, size_t nb) {
     return na && nb && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
@@ -74,6 +80,7 @@ int guard_embed(const void *d_tokens, int token_bits, int64_t tokens, const void
     if (!d_tokens || !d_out || (!d_table && rows > 0)) return call_error(GUARD_ERR_ARG, "d_tokens, d_table or d_out is NULL");
     const size_t b = dtype_bytes(dtype);
     if (!on(d_tokens, token_bits / 8) || !on(d_table, b) || !on(d_out, b)) return call_error(GUARD_ERR_ARG, "a pointer is not aligned to its elements");
+    if (!good_word(d_status, "d_status")) return GUARD_ERR_ARG;
     const size_t nout = (size_t)tokens * width * b;
     if (overlap(d_out, nout, d_tokens, (size_t)tokens * token_bits / 8) || overlap(d_out, nout, d_table, rows ? ((size_t)(rows - 1) * stride + width) * b : 0))
         return call_error(GUARD_ERR_ARG, "d_out overlaps an input");
@@ -110,6 +117,7 @@ int guard_embed_grad(const void *d_grad, int64_t stride, int dtype, const void *
     if (!d_dtable || (tokens > 0 && (!d_grad || !d_tokens))) return call_error(GUARD_ERR_ARG, "d_grad, d_tokens or d_dtable is NULL");
     const size_t b = dtype_bytes(dtype);
     if (!on(d_tokens, token_bits / 8) || !on(d_grad, b) || !on(d_dtable, b)) return call_error(GUARD_ERR_ARG, "a pointer is not aligned to its elements");
+    if (!good_word(d_status, "d_status")) return GUARD_ERR_ARG;
     const size_t nout = (size_t)rows * width * b;
     if (overlap(d_dtable, nout, d_tokens, (size_t)tokens * token_bits / 8) || overlap(d_dtable, nout, d_grad, tokens ? ((size_t)(tokens - 1) * stride + width) * b : 0) ||
         overlap(d_dtable, nout, d_workspace, need))
@@ -159,6 +167,7 @@ static int xent_check(const XentArgs &a, size_t need, size_t given, const void *
     if (need == 0 || a.x_stride < a.width || a.w_stride < a.width || a.x_stride % 8 || a.w_stride % 8 || a.x_stride >= (1LL << 36) || a.w_stride >= (1LL << 36))
         return call_error(GUARD_ERR_ARG, "invalid sizes: need 1 <= vocab <= 2^30, rows <= 2^26, width a multiple of 8 up to 2^24, strides multiples of 8 and >= width, and a product that tiles");
     if (!a.x || !a.w || !a.targets) return call_error(GUARD_ERR_ARG, "d_x, d_w or d_targets is NULL");
+    if (!good_word(a.status, "d_status")) return GUARD_ERR_ARG;
     if (!on(a.x, 16) || !on(a.w, 16) || !on(a.targets, a.target_bits / 8)) return call_error(GUARD_ERR_ARG, "d_x and d_w must be 16-byte aligned, d_targets to its elements");
     if (!a.workspace || !on(a.workspace, 256) || given < need)
         return call_error(GUARD_ERR_WORKSPACE, "workspace must be non-NULL, 256-byte aligned and at least %zu bytes", need);
@@ -363,6 +372,7 @@ int guard_adamw_create(guard_adamw **out, const guard_adamw_tensor *tensors, int
 int guard_adamw_step(guard_adamw *opt, double lr, const float *d_lr, const float *d_grad_scale, void *stream) {
     if (!opt) return call_error(GUARD_ERR_ARG, "opt is NULL");
     if (!d_lr && !std::isfinite(lr)) return call_error(GUARD_ERR_ARG, "lr is not finite");
+    if (!good_word(d_lr, "d_lr") || !good_word(d_grad_scale, "d_grad_scale")) return GUARD_ERR_ARG;
     AdamwArgs a = opt->a;
     a.lr = lr;
     a.d_lr = d_lr;

@@ -76,3 +76,15 @@ def test_a_wait_that_runs_out_is_reported_and_later_calls_work(ops, n, d, v, lim
         assert torch.equal(again["loss"], want["loss"]) and torch.equal(again_back["dx"], back["dx"]) and torch.equal(again_back["dw"], back["dw"])
     if limit == 1:
         assert ran_out == 10
+
+
+def test_adamw_refuses_scalars_off_their_alignment(ops):
+    p, grad = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    opt = ops.AdamW([p], [grad])
+    two = torch.ones(2, device="cuda")
+    step, stream = ops.lib().guard_adamw_step, torch.cuda.current_stream().cuda_stream
+    assert step(opt._h, 0.0, two.data_ptr() + 2, None, stream) == -1
+    assert step(opt._h, 1e-3, None, two.data_ptr() + 1, stream) == -1
+    assert opt.steps() == 0 and (p == 1).all()
+    assert step(opt._h, 0.0, two.data_ptr() + 4, two.data_ptr(), stream) == 0
+    assert opt.steps() == 1

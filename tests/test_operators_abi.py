@@ -126,3 +126,15 @@ def test_wait_limit_refusals(L):
     with pytest.raises(ops.GuardError):
         ops.debug_set_wait_limit(-5)
     ops.debug_set_wait_limit(0)
+
+
+def test_scalars_must_be_aligned(L):
+    """A float32 or a status word that the kernels access must lie on four bytes."""
+    assert L.guard_embed(P, 64, 4, Q, 8, 16, 16, 1, 1.0, WS, WS + (1 << 30) + 2, None) == -1
+    assert "status" in text(L)
+    assert L.guard_embed_grad(P, 16, 1, P + (1 << 30), 64, 100, 50, 16, 1.0, -1, 0, Q, WS, 1 << 30, P + (1 << 31) + 1, None) == -1
+    big = 1 << 40
+    assert L.guard_linear_xent(P, 64, Q, 64, 300, 64, 1000, 1, WS, 64, -100, WS + big, WS + big + 4096, WS + 2 * big, 1 << 30, WS + 3 * big + 2, None) == -1
+    assert L.guard_linear_xent_grad(P, 64, Q, 64, 300, 64, 1000, 1, WS, 64, -100, WS + big, WS + big + 4096, 1, WS + 2 * big, WS + 3 * big, WS + 4 * big, 1 << 30,
+                                    WS + 5 * big + 3, None) == -1
+    assert "status" in text(L)
