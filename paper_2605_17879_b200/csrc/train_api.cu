@@ -122,6 +122,9 @@ int guard_embed_grad(const void *d_grad, int64_t stride, int dtype, const void *
     if (overlap(d_dtable, nout, d_tokens, (size_t)tokens * token_bits / 8) || overlap(d_dtable, nout, d_grad, tokens ? ((size_t)(tokens - 1) * stride + width) * b : 0) ||
         overlap(d_dtable, nout, d_workspace, need))
         return call_error(GUARD_ERR_ARG, "d_dtable overlaps an input or the workspace");
+    if (d_workspace && (overlap(d_workspace, need, d_tokens, (size_t)tokens * token_bits / 8) ||
+                        overlap(d_workspace, need, d_grad, tokens ? ((size_t)(tokens - 1) * stride + width) * b : 0)))
+        return call_error(GUARD_ERR_ARG, "an input overlaps the workspace");
     if (!d_workspace || !on(d_workspace, 256) || workspace_bytes < need)
         return call_error(GUARD_ERR_WORKSPACE, "workspace must be non-NULL, 256-byte aligned and at least %zu bytes", need);
     if (tokens == 0 && accumulate) return GUARD_OK;
@@ -172,10 +175,12 @@ static int xent_check(const XentArgs &a, size_t need, size_t given, const void *
     if (!a.workspace || !on(a.workspace, 256) || given < need)
         return call_error(GUARD_ERR_WORKSPACE, "workspace must be non-NULL, 256-byte aligned and at least %zu bytes", need);
     const struct { const void *p; size_t n; } ins[] = {{a.x, ((size_t)(a.rows - 1) * a.x_stride + a.width) * 2}, {a.w, ((size_t)(a.vocab - 1) * a.w_stride + a.width) * 2},
-                                                       {a.targets, (size_t)a.rows * a.target_bits / 8}, {a.workspace, need},
-                                                       {a.lse, (size_t)a.rows * 4}, {a.grad_loss, a.grad_stride ? (size_t)a.rows * 4 : 4}};
-    for (const auto &in : ins)
+                                                       {a.targets, (size_t)a.rows * a.target_bits / 8}, {a.lse, (size_t)a.rows * 4},
+                                                       {a.grad_loss, a.grad_stride ? (size_t)a.rows * 4 : 4}, {a.workspace, need}};
+    for (const auto &in : ins) {
         if (in.p && (overlap(out0, out0 ? n0 : 0, in.p, in.n) || overlap(out1, out1 ? n1 : 0, in.p, in.n))) return call_error(GUARD_ERR_ARG, "an output overlaps an input or the workspace");
+        if (in.p && &in != &ins[5] && overlap(a.workspace, need, in.p, in.n)) return call_error(GUARD_ERR_ARG, "an input overlaps the workspace");
+    }
     if (out0 && out1 && overlap(out0, n0, out1, n1)) return call_error(GUARD_ERR_ARG, "the outputs overlap");
     return GUARD_OK;
 }

@@ -138,3 +138,23 @@ def test_scalars_must_be_aligned(L):
     assert L.guard_linear_xent_grad(P, 64, Q, 64, 300, 64, 1000, 1, WS, 64, -100, WS + big, WS + big + 4096, 1, WS + 2 * big, WS + 3 * big, WS + 4 * big, 1 << 30,
                                     WS + 5 * big + 3, None) == -1
     assert "status" in text(L)
+
+
+def test_inputs_must_not_lie_in_the_workspace(L):
+    need = L.guard_embed_grad_workspace_bytes(100, 50, 16)
+    def embed(grad=P, tokens=P + (1 << 30), out=Q, ws=WS):
+        return L.guard_embed_grad(grad, 16, 1, tokens, 64, 100, 50, 16, 1.0, -1, 0, out, ws, need, None, None)
+    assert embed(grad=WS + 512) == -1 and embed(tokens=WS + need - 8) == -1 and embed(tokens=WS - 8) == -1
+    assert "workspace" in text(L)
+    big = 1 << 40
+    need = {g: L.guard_linear_xent_workspace_bytes(300, 64, 1000, g) for g in (0, 1)}
+    def forward(x=P, w=Q, t=WS):
+        return L.guard_linear_xent(x, 64, w, 64, 300, 64, 1000, 1, t, 64, -100, WS + big, WS + big + 4096, WS + 2 * big, need[0], None, None)
+    def backward(x=P, w=Q, t=WS, lse=WS + big, g=WS + big + 4096):
+        return L.guard_linear_xent_grad(x, 64, w, 64, 300, 64, 1000, 1, t, 64, -100, lse, g, 1, WS + 2 * big, WS + 3 * big, WS + 4 * big, need[1], None, None)
+    for name in ("x", "w", "t"):
+        for at in (0, 256):
+            assert forward(**{name: WS + 2 * big + at}) == -1 and "workspace" in text(L), name
+    for name in ("x", "w", "t", "lse", "g"):
+        for at in (0, 256):
+            assert backward(**{name: WS + 4 * big + at}) == -1 and "workspace" in text(L), name
