@@ -163,12 +163,16 @@ int guard_debug_set_operator_wait_limit(long long cycles) {
     g_wait_limit.store(cycles, std::memory_order_relaxed);
     return GUARD_OK;
 }
+static int xent_sizes() {
+    return call_error(GUARD_ERR_ARG, "invalid sizes: need 1 <= vocab <= 2^30, rows <= 2^26, width a multiple of 8 up to 2^24, strides multiples of 8 and >= width, and a product that tiles");
+}
+
 // The checks that both directions share; 0 or an error.
 static int xent_check(const XentArgs &a, size_t need, size_t given, const void *out0, size_t n0, const void *out1, size_t n1) {
     if ((a.dtype != GUARD_BF16 && a.dtype != GUARD_F16) || (a.target_bits != 32 && a.target_bits != 64))
         return call_error(GUARD_ERR_ARG, "dtype must be GUARD_BF16 or GUARD_F16, target_bits 32 or 64");
     if (need == 0 || a.x_stride < a.width || a.w_stride < a.width || a.x_stride % 8 || a.w_stride % 8 || a.x_stride >= (1LL << 36) || a.w_stride >= (1LL << 36))
-        return call_error(GUARD_ERR_ARG, "invalid sizes: need 1 <= vocab <= 2^30, rows <= 2^26, width a multiple of 8 up to 2^24, strides multiples of 8 and >= width, and a product that tiles");
+        return xent_sizes();
     if (!a.x || !a.w || !a.targets) return call_error(GUARD_ERR_ARG, "d_x, d_w or d_targets is NULL");
     if (!good_word(a.status, "d_status")) return GUARD_ERR_ARG;
     if (!on(a.x, 16) || !on(a.w, 16) || !on(a.targets, a.target_bits / 8)) return call_error(GUARD_ERR_ARG, "d_x and d_w must be 16-byte aligned, d_targets to its elements");
@@ -189,7 +193,7 @@ int guard_linear_xent(const void *d_x, int64_t x_stride, const void *d_w, int64_
                       int64_t vocab, int dtype, const void *d_targets, int target_bits, int64_t ignore_index,
                       float *d_loss, float *d_lse, void *d_workspace, size_t workspace_bytes, uint32_t *d_status,
                       void *stream) {
-    if (rows == 0 && vocab >= 1 && width >= 8 && width % 8 == 0) return GUARD_OK;
+    if (rows == 0 && guard_linear_xent_workspace_bytes(1, width, vocab, 0) != 0) return GUARD_OK;
     XentArgs a{};
     a.x = d_x;
     a.w = d_w;
@@ -220,9 +224,13 @@ int guard_linear_xent_grad(const void *d_x, int64_t x_stride, const void *d_w, i
     if (grad_stride != 0 && grad_stride != 1) return call_error(GUARD_ERR_ARG, "grad_stride must be 0 or 1");
     if (!d_dx && !d_dw) return call_error(GUARD_ERR_ARG, "d_dx and d_dw are both NULL");
     if (!on(d_dx, 16) || !on(d_dw, 16)) return call_error(GUARD_ERR_ARG, "d_dx and d_dw must be 16-byte aligned");
-    if (rows == 0 && vocab >= 1 && width >= 8 && width % 8 == 0 && (dtype == GUARD_BF16 || dtype == GUARD_F16)) {
+    if (rows == 0 && (dtype == GUARD_BF16 || dtype == GUARD_F16)) {       // dw is all there is to write
+        if (guard_linear_xent_workspace_bytes(1, width, vocab, 1) == 0 || w_stride < width || w_stride % 8 || w_stride >= (1LL << 36)) return xent_sizes();
         if (!d_dw) return GUARD_OK;
-        const cudaError_t e = cudaMemsetAsync(d_dw, 0, (size_t)vocab * width * 2, (cudaStream_t)stream);
+        const size_t ndw = (size_t)vocab * width * 2;
+        if ((d_w && overlap(d_dw, ndw, d_w, ((size_t)(vocab - 1) * w_stride + width) * 2)) || overlap(d_dw, ndw, d_workspace, workspace_bytes))
+            return call_error(GUARD_ERR_ARG, "an output overlaps an input or the workspace");
+        const cudaError_t e = cudaMemsetAsync(d_dw, 0, ndw, (cudaStream_t)stream);
         if (e == cudaSuccess) return GUARD_OK;
         (void)cudaGetLastError();
         return call_error(GUARD_ERR_CUDA, "cudaMemsetAsync: %s", cudaGetErrorString(e));

@@ -158,3 +158,16 @@ def test_inputs_must_not_lie_in_the_workspace(L):
     for name in ("x", "w", "t", "lse", "g"):
         for at in (0, 256):
             assert backward(**{name: WS + 4 * big + at}) == -1 and "workspace" in text(L), name
+
+
+def test_no_rows_of_an_impossible_product(L):
+    """Without rows dw is all there is to clear: its size has to be one that a call with rows would take."""
+    big = 1 << 40
+    def backward(d=64, v=1000, w=Q, wst=64, dw=WS + 3 * big):
+        return L.guard_linear_xent_grad(P, d, w, wst, 0, d, v, 1, WS, 64, -100, WS + big, WS + big + 4096, 1, None, dw, WS + 4 * big, 1 << 30, None, None)
+    for bad in (dict(v=1 << 62), dict(v=1 << 60), dict(v=(1 << 30) + 8), dict(d=1 << 25, wst=1 << 25), dict(wst=56), dict(wst=68), dict(dw=Q + 160), dict(dw=WS + 4 * big)):
+        assert backward(**bad) == -1, bad
+        assert text(L)
+    def forward(d=64, v=1000):
+        return L.guard_linear_xent(P, d, Q, d, 0, d, v, 1, WS, 64, -100, WS + big, WS + big + 4096, WS + 2 * big, 1 << 30, None, None)
+    assert forward() == 0 and forward(v=1 << 62) == -1 and forward(d=1 << 25) == -1
