@@ -58,6 +58,16 @@ bool good_word(const void *p, const char *name) {
     call_error(GUARD_ERR_ARG, "%s is not aligned to its four bytes", name);
     return false;
 }
+// Whether the stream is being captured (a graph would copy from or to host memory that is gone when it is replayed).
+int not_capturing(void *stream, const char *what) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    const cudaError_t e = cudaStreamIsCapturing((cudaStream_t)stream, &status);
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();
+        return call_error(GUARD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+    }
+    return status == cudaStreamCaptureStatusNone ? GUARD_OK : call_error(GUARD_ERR_ARG, "%s cannot be captured into a graph", what);
+}
 bool overlap(const void *a, size_t na, const void *b, size_t nb) {
     return na && nb && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
@@ -345,6 +355,8 @@ int guard_adamw_create(guard_adamw **out, const guard_adamw_tensor *tensors, int
             while (i + 1 < n && table[i + 1].first <= c * kAdamwChunk) ++i;
             map[c] = (uint32_t)i;
         }
+        const int free = not_capturing(stream, "guard_adamw_create");
+        if (free != GUARD_OK) return free;
         guard_adamw *o = new guard_adamw();
         o->grad_dtype = grad_dtype;
         o->copy_dtype = copy_dtype;
@@ -395,6 +407,8 @@ int guard_adamw_step(guard_adamw *opt, double lr, const float *d_lr, const float
 
 int guard_adamw_steps(guard_adamw *opt, int64_t *steps, void *stream) {
     if (!opt || !steps) return call_error(GUARD_ERR_ARG, "opt or steps is NULL");
+    const int free = not_capturing(stream, "guard_adamw_steps");
+    if (free != GUARD_OK) return free;
     cudaError_t e = cudaMemcpyAsync(steps, &opt->a.counter->step, sizeof *steps, cudaMemcpyDeviceToHost, (cudaStream_t)stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
     if (e == cudaSuccess) return GUARD_OK;

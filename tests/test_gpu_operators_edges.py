@@ -88,3 +88,23 @@ def test_adamw_refuses_scalars_off_their_alignment(ops):
     assert opt.steps() == 0 and (p == 1).all()
     assert step(opt._h, 0.0, two.data_ptr() + 4, two.data_ptr(), stream) == 0
     assert opt.steps() == 1
+
+
+def test_adamw_is_not_made_or_asked_inside_a_capture(ops):
+    """Making an optimiser copies its table from host memory, asking for its steps copies to it: neither address lives when a
+    graph is replayed.  The capture itself goes on."""
+    p, grad = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    opt = ops.AdamW([p], [grad])
+    opt.step(1e-3)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(ops.GuardError):
+            ops.AdamW([torch.ones(8, device="cuda")], [torch.ones(8, device="cuda")])
+        with pytest.raises(ops.GuardError):
+            opt.steps()
+        opt.step(1e-3)
+    assert opt.steps() == 1
+    graph.replay()
+    graph.replay()
+    assert opt.steps() == 3
