@@ -97,12 +97,11 @@ struct SortShared {
 
 // A token's key: the token, or `rows` (behind all tokens) where it adds nothing.
 __device__ __forceinline__ uint32_t key_of(const EmbedGradArgs &a, int64_t t) {
-    if (t == a.padding) return (uint32_t)a.rows;
     if (t < 0 || t >= a.rows) {
         if (a.status) atomicOr(a.status, kStatIndex);
         return (uint32_t)a.rows;
     }
-    return (uint32_t)t;
+    return t == a.padding ? (uint32_t)a.rows : (uint32_t)t;
 }
 __device__ __forceinline__ uint32_t key_at(const EmbedGradArgs &a, int64_t i) { return key_of(a, token_at(a.tokens, a.token_bits, i)); }
 

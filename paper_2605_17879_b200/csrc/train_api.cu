@@ -152,8 +152,6 @@ int guard_embed_grad(const void *d_grad, int64_t stride, int dtype, const void *
     a.dtable = d_dtable;
     a.workspace = d_workspace;
     a.status = d_status;
-    // (padding -1: a token of -1 is an error, not padding)
-    if (padding_idx < 0) a.padding = INT64_MIN;
     return launched(launch_embed_grad(a, dtype, (cudaStream_t)stream), "embedding gradient");
 }
 

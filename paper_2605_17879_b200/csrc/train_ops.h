@@ -101,7 +101,7 @@ struct EmbedGradArgs {
     int64_t stride;
     const void *tokens;
     int token_bits;
-    int64_t n, rows, width, padding;
+    int64_t n, rows, width, padding;   // padding: a row, or -1
     float scale;
     int accumulate;
     void *dtable;

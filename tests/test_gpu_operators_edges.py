@@ -108,3 +108,17 @@ def test_adamw_is_not_made_or_asked_inside_a_capture(ops):
     graph.replay()
     graph.replay()
     assert opt.steps() == 3
+
+
+@pytest.mark.parametrize("n", [6, 9000])
+@pytest.mark.parametrize("token", [-1, -2 ** 63, 2 ** 63 - 1, 4])
+def test_every_token_outside_the_table_is_an_error(ops, n, token):
+    grad = torch.ones(n, 8, device="cuda")
+    ids = torch.arange(n, device="cuda") % 4
+    ids[5] = token
+    for padding in (-1, 2):
+        out = {"dtable": torch.empty(4, 8, device="cuda"), "status": torch.zeros(1, dtype=torch.uint32, device="cuda")}
+        ops.embed_grad(grad, ids, 4, padding_idx=padding, out=out)
+        assert int(out["status"].item()) == ops.STATUS_INDEX
+        want = [float(((ids == v) & (v != padding)).sum()) for v in range(4)]
+        assert out["dtable"][:, 0].tolist() == want
