@@ -12,6 +12,7 @@ as out["status"].  The first call on a device makes that word and waits for it: 
 from __future__ import annotations
 
 import ctypes as C
+import threading
 from typing import Dict, Optional, Sequence
 
 import torch
@@ -91,24 +92,33 @@ def _contiguous(t: torch.Tensor, what: str, dtype: torch.dtype, numel: int, devi
 
 
 _status: Dict[int, torch.Tensor] = {}
+_status_lock = threading.Lock()
 _nat = None
 
 
-def _call(name, first, *args):
-    """A native call, its device's status word in place before: the mapping of outputs."""
+def _make_status(dev: int, device) -> None:
+    """The status word of a device: made once, by whichever thread comes first."""
     global _nat
-    if not isinstance(first, torch.Tensor) or not first.is_cuda:
-        raise ValueError("expected CUDA tensors")
-    dev = first.get_device()
-    if dev not in _status:
+    with _status_lock:
+        if dev in _status:
+            return
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("make the first call on a device before capturing")
         lib()
-        word = torch.zeros(1, dtype=torch.int32, device=first.device)
+        word = torch.zeros(1, dtype=torch.int32, device=device)
         torch.cuda.current_stream(dev).synchronize()      # any stream may use it from now on
         _nat = guard._native()
         _nat.set_status(dev, word.data_ptr())
         _status[dev] = word
+
+
+def _call(name, first, *args):
+    """A native call, its device's status word in place before: the mapping of outputs."""
+    if not isinstance(first, torch.Tensor) or not first.is_cuda:
+        raise ValueError("expected CUDA tensors")
+    dev = first.get_device()
+    if dev not in _status:
+        _make_status(dev, first.device)
     r = getattr(_nat, name)(first, *args)
     if r.__class__ is int:
         _check(r)
