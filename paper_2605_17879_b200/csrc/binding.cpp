@@ -319,6 +319,8 @@ PyObject *py_set_status(PyObject *, PyObject *const *args, Py_ssize_t n) {
 // A call's tensors: checks that set a Python error and return false, and outputs made or taken from the caller's mapping.
 struct Call {
     int device = -1;
+    at::Tensor kept[8];        // what the caller's mapping held, which other threads may change while the GIL is released
+    int n_kept = 0;
     const at::Tensor *cuda(PyObject *o, const char *what) {
         if (!THPVariable_Check(o) || !THPVariable_Unpack(o).is_cuda()) {
             PyErr_Format(PyExc_ValueError, "%s must be a CUDA tensor", what);
@@ -367,6 +369,7 @@ struct Call {
             PyErr_Format(PyExc_ValueError, "%s must be contiguous, of %s and of %lld elements", what, c10::toString(type), (long long)numel);
             return false;
         }
+        kept[n_kept++] = *t;
         *to = t->data_ptr();
         return true;
     }
@@ -452,8 +455,12 @@ PyObject *py_embed(PyObject *, PyObject *const *args, Py_ssize_t n) {
         void *to;
         uint32_t *status;
         if (!made.o || !c.output(args[3], made.o, "out", table->scalar_type(), size, false, &to) || !c.status(args[3], &status)) return nullptr;
-        const int rc = guard_embed(tokens->data_ptr(), bits, tokens->numel(), table->data_ptr(), table->size(0), width, stride, code, (float)scale, to,
-                                   status, here.stream);
+        const void *ids = tokens->data_ptr(), *from = table->data_ptr();
+        const int64_t count = tokens->numel(), rows = table->size(0);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = guard_embed(ids, bits, count, from, rows, width, stride, code, (float)scale, to, status, here.stream);
+        Py_END_ALLOW_THREADS
         return result(rc, args[3], made);
     } catch (const std::exception &e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
@@ -498,8 +505,11 @@ PyObject *py_embed_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
         if (!made.o || !c.output(args[7], made.o, "dtable", grad.scalar_type(), {rows, width}, false, &to) || !c.workspace(args[6], need, keep, &ws, &bytes) ||
             !c.status(args[7], &status))
             return nullptr;
-        const int rc = guard_embed_grad(grad.data_ptr(), stride, code, tokens->data_ptr(), bits, count, rows, width, (float)scale, padding, accumulate, to, ws, bytes,
-                                        status, here.stream);
+        const void *from = grad.data_ptr(), *ids = tokens->data_ptr();
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = guard_embed_grad(from, stride, code, ids, bits, count, rows, width, (float)scale, padding, accumulate, to, ws, bytes, status, here.stream);
+        Py_END_ALLOW_THREADS
         return result(rc, args[7], made);
     } catch (const std::exception &e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
@@ -511,6 +521,7 @@ PyObject *py_embed_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
 struct Product {
     const at::Tensor *x = nullptr, *w = nullptr, *targets = nullptr;
     int bits = 0, code = -1;
+    const void *px = nullptr, *pw = nullptr, *pt = nullptr;
     int64_t xs = -1, ws = -1, rows = 0, width = 0, vocab = 0;
     bool read(Call &c, PyObject *const *args) {
         if (!(x = c.cuda(args[0], "x")) || !(w = c.cuda(args[1], "w")) || !(targets = c.cuda(args[2], "targets")) || !(bits = Call::token_bits(*targets, "targets")) ||
@@ -522,6 +533,7 @@ struct Product {
         }
         if ((xs = Call::rows(*x, "x")) < 0 || (ws = Call::rows(*w, "w")) < 0) return false;
         rows = x->size(0), width = x->size(1), vocab = w->size(0);
+        px = x->data_ptr(), pw = w->data_ptr(), pt = targets->data_ptr();
         if (w->size(1) != width || targets->numel() != rows) {
             PyErr_SetString(PyExc_ValueError, "need x [rows, width], w [vocab, width] and rows targets");
             return false;
@@ -547,8 +559,11 @@ PyObject *py_linear_xent(PyObject *, PyObject *const *args, Py_ssize_t n) {
         if (!made.o || !c.output(args[5], made.o, "loss", c10::kFloat, {p.rows}, false, &loss) || !c.output(args[5], made.o, "lse", c10::kFloat, {p.rows}, false, &lse) ||
             !c.workspace(args[4], guard_linear_xent_workspace_bytes(p.rows, p.width, p.vocab, 0), keep, &ws, &bytes) || !c.status(args[5], &status))
             return nullptr;
-        const int rc = guard_linear_xent(p.x->data_ptr(), p.xs, p.w->data_ptr(), p.ws, p.rows, p.width, p.vocab, p.code, p.targets->data_ptr(), p.bits, ignore,
-                                         (float *)loss, (float *)lse, ws, bytes, status, here.stream);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = guard_linear_xent(p.px, p.xs, p.pw, p.ws, p.rows, p.width, p.vocab, p.code, p.pt, p.bits, ignore, (float *)loss, (float *)lse, ws, bytes, status,
+                               here.stream);
+        Py_END_ALLOW_THREADS
         return result(rc, args[5], made);
     } catch (const std::exception &e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
@@ -578,8 +593,11 @@ PyObject *py_linear_xent_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
             !c.output(args[7], made.o, "dw", p.w->scalar_type(), {p.vocab, p.width}, true, &dw) ||
             !c.workspace(args[6], guard_linear_xent_workspace_bytes(p.rows, p.width, p.vocab, 1), keep, &ws, &bytes) || !c.status(args[7], &status))
             return nullptr;
-        const int rc = guard_linear_xent_grad(p.x->data_ptr(), p.xs, p.w->data_ptr(), p.ws, p.rows, p.width, p.vocab, p.code, p.targets->data_ptr(), p.bits, ignore,
-                                              (const float *)lse, (const float *)g, one ? 0 : 1, dx, dw, ws, bytes, status, here.stream);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = guard_linear_xent_grad(p.px, p.xs, p.pw, p.ws, p.rows, p.width, p.vocab, p.code, p.pt, p.bits, ignore, (const float *)lse, (const float *)g,
+                                    one ? 0 : 1, dx, dw, ws, bytes, status, here.stream);
+        Py_END_ALLOW_THREADS
         return result(rc, args[7], made);
     } catch (const std::exception &e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());

@@ -122,3 +122,42 @@ def test_every_token_outside_the_table_is_an_error(ops, n, token):
         assert int(out["status"].item()) == ops.STATUS_INDEX
         want = [float(((ids == v) & (v != padding)).sum()) for v in range(4)]
         assert out["dtable"][:, 0].tolist() == want
+
+
+GIL_STUB = r"""
+#include <stddef.h>
+extern int PyGILState_Check(void);
+static int held;
+int stub_held(void) { return held; }
+#define STUB(name) int name() { held += PyGILState_Check(); return 0; }
+STUB(guard_embed) STUB(guard_embed_grad) STUB(guard_linear_xent) STUB(guard_linear_xent_grad)
+"""
+GIL_CALLS = r"""
+import ctypes, sys, torch
+from paper_2605_17879_b200 import operators as ops
+held = ctypes.CDLL(sys.argv[1]).stub_held
+x = torch.zeros(4, 8, dtype=torch.bfloat16, device="cuda")
+t = torch.zeros(4, dtype=torch.int64, device="cuda")
+f = torch.zeros(4, device="cuda")
+got = []
+for call in (lambda: ops.embed(t, x), lambda: ops.embed_grad(x, t, 4), lambda: ops.linear_xent(x, x, t), lambda: ops.linear_xent_grad(x, x, t, f, f)):
+    before = held()
+    call()
+    got.append(held() - before)
+print("held", got)
+"""
+
+
+def test_native_calls_release_the_interpreter_lock(tmp_path):
+    """The library's entries are replaced by ones that say whether the calling thread holds the lock."""
+    import os
+    import subprocess
+    import sys
+    (tmp_path / "stub.c").write_text(GIL_STUB)
+    so = str(tmp_path / "stub.so")
+    subprocess.check_call(["gcc", "-shared", "-fPIC", "-o", so, str(tmp_path / "stub.c")])
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", GIL_CALLS, so], cwd=root, env=dict(os.environ, LD_PRELOAD=so, PYTHONPATH=root), capture_output=True, text=True,
+                       timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+    assert "held [0, 0, 0, 0]" in r.stdout, r.stdout
