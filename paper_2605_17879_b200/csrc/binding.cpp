@@ -395,7 +395,12 @@ struct Call {
             PyErr_Format(PyExc_ValueError, "out['%s'] is missing", name);
             return false;
         }
-        return flat(v.o, name, type, numel, to);
+        return flat(v.o, name, type, numel, to) && wrote(kept[n_kept - 1]);
+    }
+    // Tells autograd that a tensor's values change, as torch's own in-place operations do.
+    static bool wrote(const at::Tensor &t) {
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+        return true;
     }
     bool workspace(PyObject *given, size_t need, at::Tensor &keep, void **p, size_t *bytes) {
         if (given == Py_None) {
@@ -605,6 +610,20 @@ PyObject *py_linear_xent_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
     }
 }
 
+// wrote(tuple of tensors): they have been written in place
+PyObject *py_wrote(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (!want_args(n, 1)) return nullptr;
+    if (!PyTuple_CheckExact(args[0])) {
+        PyErr_SetString(PyExc_TypeError, "expected a tuple");
+        return nullptr;
+    }
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(args[0]); ++i) {
+        PyObject *o = PyTuple_GET_ITEM(args[0], i);
+        if (THPVariable_Check(o)) Call::wrote(THPVariable_Unpack(o));
+    }
+    Py_RETURN_NONE;
+}
+
 PyMethodDef g_methods[] = {{"current_stream", (PyCFunction)(void (*)(void))py_current_stream, METH_FASTCALL, nullptr},
                            {"ingest", (PyCFunction)(void (*)(void))py_ingest, METH_FASTCALL, nullptr},
                            {"score", (PyCFunction)(void (*)(void))py_score, METH_FASTCALL, nullptr},
@@ -616,6 +635,7 @@ PyMethodDef g_methods[] = {{"current_stream", (PyCFunction)(void (*)(void))py_cu
                            {"embed_grad", (PyCFunction)(void (*)(void))py_embed_grad, METH_FASTCALL, nullptr},
                            {"linear_xent", (PyCFunction)(void (*)(void))py_linear_xent, METH_FASTCALL, nullptr},
                            {"linear_xent_grad", (PyCFunction)(void (*)(void))py_linear_xent_grad, METH_FASTCALL, nullptr},
+                           {"wrote", (PyCFunction)(void (*)(void))py_wrote, METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_guard_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -224,6 +224,8 @@ class AdamW:
                 state = {k: torch.zeros(blocks * per, dtype=t, device=dev) for k, (t, per) in kinds.items()}
             at = {k: _contiguous(state[k], "state[%r]" % k, t, blocks * per, dev) for k, (t, per) in kinds.items()}
             self.state = {k: state[k] for k in kinds}
+            self._written = (*self.params, *(self.copies or ()), *self.state.values())
+            self._wrote = guard._native().wrote
             self._ws = torch.empty(max(256, int(lib().guard_adamw_workspace_bytes(table, n))), dtype=torch.uint8, device=dev)
             _check(lib().guard_adamw_create(C.byref(self._h), table, n, gcode, ccode, state_bits, betas[0], betas[1], eps, at["m"], at["v"],
                                             at.get("m_scale"), at.get("v_scale"), step, seed & 0xFFFFFFFF, self._ws.data_ptr(),
@@ -240,6 +242,7 @@ class AdamW:
             dlr = _contiguous(lr, "lr", torch.float32, 1, self.device) if isinstance(lr, torch.Tensor) else None
             gs = _contiguous(grad_scale, "grad_scale", torch.float32, 1, self.device) if grad_scale is not None else None
             _check(lib().guard_adamw_step(self._h, 0.0 if dlr else lr, dlr, gs, guard._stream()))
+        self._wrote(self._written)            # (autograd keeps versions of them)
 
     def steps(self) -> int:
         """Updates made so far (synchronises)."""

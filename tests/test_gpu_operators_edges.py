@@ -161,3 +161,46 @@ def test_native_calls_release_the_interpreter_lock(tmp_path):
                        timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
     assert "held [0, 0, 0, 0]" in r.stdout, r.stdout
+
+
+def test_autograd_notices_what_the_operators_overwrite(ops):
+    """A tensor that a backward pass still needs and that a call has written into since: torch refuses it, as it does after its
+    own in-place operations."""
+    g = gen(3)
+    x, w = torch.randn(4, 8, generator=g, device="cuda").bfloat16(), torch.randn(16, 8, generator=g, device="cuda").bfloat16()
+    t = torch.tensor([1, 5, 5, 2], device="cuda")
+    first = ops.linear_xent(x, w, t)
+    one = torch.ones(1, device="cuda")
+
+    def refused(buffer, call):
+        leaf = torch.ones((), dtype=buffer.dtype, device="cuda", requires_grad=True)
+        y = (buffer * leaf).sum()
+        call()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+    out = torch.empty(4, 8, dtype=torch.bfloat16, device="cuda")
+    refused(out, lambda: ops.embed(t, w, out={"out": out}))
+    table = torch.zeros(16, 8, dtype=torch.bfloat16, device="cuda")
+    refused(table, lambda: ops.embed_grad(x, t, 16, accumulate=True, out={"dtable": table}))
+    for name in ("loss", "lse"):
+        refused(first[name], lambda: ops.linear_xent(x, w, t, out=first))
+    back = ops.linear_xent_grad(x, w, t, first["lse"], one)
+    for name in ("dx", "dw"):
+        refused(back[name], lambda: ops.linear_xent_grad(x, w, t, first["lse"], one, out=back))
+    p, copy = torch.ones(300, device="cuda"), torch.ones(300, device="cuda").bfloat16()
+    opt = ops.AdamW([p], [torch.ones(300, device="cuda")], copies=[copy])
+    for buffer in (p, copy, opt.state["m"]):
+        refused(buffer, lambda: opt.step(1e-3))
+    # inputs are not written, and what inference mode made has no versions
+    leaf = torch.ones((), dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    y = (x * leaf).sum()
+    ops.linear_xent_grad(x, w, t, first["lse"], one)
+    y.backward()
+    with torch.inference_mode():
+        out = torch.empty(4, 8, dtype=torch.bfloat16, device="cuda")
+        q = torch.ones(300, device="cuda")
+        ops.embed(t, w, out={"out": out})
+        opt = ops.AdamW([q], [torch.ones(300, device="cuda")])
+    ops.embed(t, w, out={"out": out})
+    opt.step(1e-3)
+    assert torch.equal(out, w[t]) and opt.steps() == 1
