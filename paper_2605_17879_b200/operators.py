@@ -220,7 +220,8 @@ class AdamW:
         kinds = {"m": (torch.float32, BLOCK), "v": (torch.float32, BLOCK)} if state_bits == 32 else {
             "m": (torch.float8_e4m3fn, BLOCK), "v": (torch.float8_e4m3fn, BLOCK), "m_scale": (torch.float32, 1), "v_scale": (torch.float32, 1)}
         with _here(dev):
-            if state is None:
+            own = state is None
+            if own:
                 state = {k: torch.zeros(blocks * per, dtype=t, device=dev) for k, (t, per) in kinds.items()}
             at = {k: _contiguous(state[k], "state[%r]" % k, t, blocks * per, dev) for k, (t, per) in kinds.items()}
             self.state = {k: state[k] for k in kinds}
@@ -230,6 +231,8 @@ class AdamW:
             _check(lib().guard_adamw_create(C.byref(self._h), table, n, gcode, ccode, state_bits, betas[0], betas[1], eps, at["m"], at["v"],
                                             at.get("m_scale"), at.get("v_scale"), step, seed & 0xFFFFFFFF, self._ws.data_ptr(),
                                             self._ws.numel(), guard._stream()))
+            # (what is allocated here is handed to others in the order of this stream alone, unless the allocator hears of more)
+            self._own, self._streams = [self._ws, *(self.state.values() if own else ())], {guard._stream()}
 
     @staticmethod
     def state_blocks(params: Sequence[torch.Tensor]) -> int:
@@ -241,7 +244,12 @@ class AdamW:
         with _here(self.device):
             dlr = _contiguous(lr, "lr", torch.float32, 1, self.device) if isinstance(lr, torch.Tensor) else None
             gs = _contiguous(grad_scale, "grad_scale", torch.float32, 1, self.device) if grad_scale is not None else None
-            _check(lib().guard_adamw_step(self._h, 0.0 if dlr else lr, dlr, gs, guard._stream()))
+            stream = guard._stream()
+            if stream not in self._streams:
+                for t in self._own:
+                    t.record_stream(torch.cuda.current_stream())
+                self._streams.add(stream)
+            _check(lib().guard_adamw_step(self._h, 0.0 if dlr else lr, dlr, gs, stream))
         self._wrote(self._written)            # (autograd keeps versions of them)
 
     def steps(self) -> int:

@@ -204,3 +204,23 @@ def test_autograd_notices_what_the_operators_overwrite(ops):
     ops.embed(t, w, out={"out": out})
     opt.step(1e-3)
     assert torch.equal(out, w[t]) and opt.steps() == 1
+
+
+def test_adamw_memory_outlives_a_step_on_another_stream(ops):
+    """An optimiser that is dropped while a step of it still runs elsewhere: what it had allocated is not handed out before that."""
+    p, grad = torch.ones(100000, device="cuda"), torch.ones(100000, device="cuda")
+    opt = ops.AdamW([p], [grad])
+    opt.step(1e-3)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)           # a fifth of a second
+        opt.step(1e-3)
+    mine = {t.data_ptr() for t in (opt._ws, *opt.state.values())}
+    sizes = [t.untyped_storage().nbytes() for t in (opt._ws, *opt.state.values())]
+    running = side.record_event()
+    del opt
+    again = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+    assert not running.query()                    # (the step is still to come)
+    assert not mine & {t.data_ptr() for t in again}
+    side.synchronize()
