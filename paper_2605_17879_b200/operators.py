@@ -189,6 +189,10 @@ class AdamW:
     state: {"m", "v"} of a flat layout, each parameter starting on a block of 256 elements (numel of a state:
     256 * state_blocks(params)); float32 for state_bits 32, and for 8 torch.float8_e4m3fn with {"m_scale", "v_scale"}, a
     float32 per block.  None: zeros.  step: updates made so far.
+
+    A step may run on any stream; it waits for the constructor's work by itself, and steps must be ordered with one another.
+    Neither the constructor nor steps() may be captured; finish the constructor's work before a step is.  A captured step
+    holds addresses: keep the object, and all that it was given, as long as the graph is replayed.
     """
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], *, betas=(0.9, 0.999), eps: float = 1e-8,
@@ -233,6 +237,7 @@ class AdamW:
                                             self._ws.numel(), guard._stream()))
             # (what is allocated here is handed to others in the order of this stream alone, unless the allocator hears of more)
             self._own, self._streams = [self._ws, *(self.state.values() if own else ())], {guard._stream()}
+            self._made = torch.cuda.current_stream().record_event()
 
     @staticmethod
     def state_blocks(params: Sequence[torch.Tensor]) -> int:
@@ -246,9 +251,12 @@ class AdamW:
             gs = _contiguous(grad_scale, "grad_scale", torch.float32, 1, self.device) if grad_scale is not None else None
             stream = guard._stream()
             if stream not in self._streams:
+                current = torch.cuda.current_stream()
                 for t in self._own:
-                    t.record_stream(torch.cuda.current_stream())
-                self._streams.add(stream)
+                    t.record_stream(current)
+                if not torch.cuda.is_current_stream_capturing():      # (a capture waits for nothing outside it)
+                    current.wait_event(self._made)
+                    self._streams.add(stream)
             _check(lib().guard_adamw_step(self._h, 0.0 if dlr else lr, dlr, gs, stream))
         self._wrote(self._written)            # (autograd keeps versions of them)
 

@@ -224,3 +224,28 @@ def test_adamw_memory_outlives_a_step_on_another_stream(ops):
     assert not running.query()                    # (the step is still to come)
     assert not mine & {t.data_ptr() for t in again}
     side.synchronize()
+
+
+def test_adamw_steps_elsewhere_behind_its_making(ops):
+    """The table of tensors and the states are made in the order of the constructor's stream; a step on another stream waits
+    for them by itself."""
+    want = torch.ones(5000, device="cuda")
+    grad = torch.full((5000,), 0.5, device="cuda")
+    opt = ops.AdamW([want], [grad])
+    opt.step(1e-2)
+    p = torch.ones(5000, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)               # a tenth of a second
+    opt = ops.AdamW([p], [grad])
+    with torch.cuda.stream(side):
+        opt.step(1e-2)
+    side.synchronize()
+    assert torch.equal(p, want) and opt.steps() == 1
+    # a capture brings its own stream, and may not wait for work outside it: everything has been waited for before
+    opt = ops.AdamW([p], [grad])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step(1e-2)
+    graph.replay()
+    assert opt.steps() == 1
