@@ -428,7 +428,9 @@ int guard_embed_grad(const void *d_grad, int64_t stride, int dtype, const void *
  *   dx = G w, [rows][width], and dw = G^T x, [vocab][width], both of type dtype.
  * d_lse: as guard_linear_xent gave it.  d_grad_loss: [rows] (grad_stride 1) or one value for all rows
  * (grad_stride 0).  One of d_dx and d_dw may be NULL.  G is held in dtype, a piece of the vocabulary at a time.
- * The workspace depends on whether gradients are wanted (grads 0 or 1).
+ * The workspace depends on whether gradients are wanted (grads 0 or 1).  For gradients it holds G of a piece (512 MB at
+ * most, or 512 bytes a row where that is more, rows rounded up to 256), a copy of x, and dx in float32 where the vocabulary
+ * takes several pieces or dx has few tiles.
  */
 size_t guard_linear_xent_workspace_bytes(int64_t rows, int64_t width, int64_t vocab, int grads);
 int guard_linear_xent(const void *d_x, int64_t x_stride, const void *d_w, int64_t w_stride, int64_t rows, int64_t width,

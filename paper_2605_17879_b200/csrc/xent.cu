@@ -895,7 +895,8 @@ struct XentLayout {
     int n_parts, max_units, max_splits;     // max_units 0: dx is written directly
 };
 
-// What G of one piece of the vocabulary may take.  More pieces cost more passes over dx's partial sums (0.3 GB a piece for
+// What G of one piece of the vocabulary may take, unless the narrowest piece, a tile of 256 entries, takes more: 512 bytes a
+// row, which is more from 2^20 rows on (2^26 rows, the most there may be: 34 GB).  More pieces cost more passes over dx's partial sums (0.3 GB a piece for
 // 8 192 x 4 096, some 50 us beside 7 ms of products); this is a quarter of the 16-bit logits of 8 192 rows and 131 072 entries.
 constexpr int64_t kPieceBytes = 512ll << 20;
 

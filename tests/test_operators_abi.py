@@ -171,3 +171,15 @@ def test_no_rows_of_an_impossible_product(L):
     def forward(d=64, v=1000):
         return L.guard_linear_xent(P, d, Q, d, 0, d, v, 1, WS, 64, -100, WS + big, WS + big + 4096, WS + 2 * big, 1 << 30, None, None)
     assert forward() == 0 and forward(v=1 << 62) == -1 and forward(d=1 << 25) == -1
+
+
+@pytest.mark.parametrize("rows,width,vocab", [(1, 8, 1), (300, 64, 1000), (8192, 4096, 131072), (40, 4096, 1 << 24), (1 << 20, 64, 5000), ((1 << 22) - 5, 128, 257), (1 << 26, 8, 300)])
+def test_workspace_of_the_gradients_is_what_is_stated(L, rows, width, vocab):
+    """G of a piece of the vocabulary (512 MB, or 512 bytes a row where that is more), a copy of x, dx in float32 where there are
+    several pieces or few tiles, and some words a row."""
+    up = lambda x, to: (x + to - 1) // to * to    # noqa: E731
+    padded, columns = up(rows, 256), up(width, 256)
+    held = max(min(512 << 20, padded * up(vocab, 256) * 2), padded * 512)
+    need = L.guard_linear_xent_workspace_bytes(rows, width, vocab, 1)
+    sums = max(padded * columns * 4, 148 // 2 * 256 * 256 * 4)
+    assert padded * 512 <= need <= held + padded * width * 2 + sums + padded * 20 + 16 * 256
