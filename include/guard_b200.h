@@ -386,6 +386,8 @@ const char *guard_last_error(const guard_ctx *ctx);
  *     contiguous and must not overlap inputs or one another.
  *   - Sums are held in float32 and every output is rounded once, to nearest.  Results are the same from
  *     call to call, bit for bit.
+ *   - Inputs must not lie in the workspace.  Pointers are aligned to their elements (d_status, d_lr and
+ *     d_grad_scale to four bytes).
  *   - Sizes of zero are allowed where a call has nothing to do or outputs to clear.
  */
 enum { GUARD_F32 = 0, GUARD_BF16 = 1, GUARD_F16 = 2 };   /* element types */
@@ -421,13 +423,15 @@ int guard_embed_grad(const void *d_grad, int64_t stride, int dtype, const void *
  * multiples of 8 elements, width a multiple of 8; rows <= 2^26.  d_targets: [rows] int32 or int64 (target_bits).  Rows whose
  * target is ignore_index are left out: loss and lse are 0, and what they hold reaches nothing.  A target
  * that is neither ignore_index nor in 0..vocab-1 sets GUARD_STATUS_INDEX, gives a loss of NaN and an lse of 0,
- * and is left out of the gradients.  Logits that are not finite give losses and gradients that are not.
+ * and is left out of the gradients.  A logit that is infinite or NaN gives a loss, or at least gradients, that are not finite.
  *
  * guard_linear_xent_grad: the gradients of sum over n of grad_loss[n] * loss[n]: with
  *   G[n][v] = grad_loss[n] * (exp(z[n][v] - lse[n]) - [v = target[n]]),
  *   dx = G w, [rows][width], and dw = G^T x, [vocab][width], both of type dtype.
+ * The logits are made again with the forward pass's own steps, so that G agrees with d_lse to its last bit.
  * d_lse: as guard_linear_xent gave it.  d_grad_loss: [rows] (grad_stride 1) or one value for all rows
- * (grad_stride 0).  One of d_dx and d_dw may be NULL.  G is held in dtype, a piece of the vocabulary at a time.
+ * (grad_stride 0).  One of d_dx and d_dw may be NULL.  G is held in dtype, a piece of the vocabulary at a time
+ * (which adds to the outputs' own rounding error: 2 % under 32 001 entries, a quarter under 100).
  * The workspace depends on whether gradients are wanted (grads 0 or 1).  For gradients it holds G of a piece (512 MB at
  * most, or 512 bytes a row where that is more, rows rounded up to 256), a copy of x, and dx in float32 where the vocabulary
  * takes several pieces or dx has few tiles.
@@ -463,7 +467,8 @@ int guard_debug_set_operator_wait_limit(long long cycles);
  * one smallest step (2^-9 of the scale) at least.  Infinite states become NaN.
  * Elements behind a tensor's end are left as they are.
  *
- * guard_adamw_create copies the table of tensors into the workspace (on `stream`, from host memory; the
+ * guard_adamw_create copies the table of tensors into the workspace (on `stream`, from host memory; an
+ * update on another stream has to be ordered behind it; the
  * addresses must stay valid until guard_adamw_destroy; parameters must not overlap one another).
  * eps >= 1e-30 (second moments below 2^-126 count as zero beside it).  `step`: updates made so far (0 for
  * new states).  guard_adamw_step makes one update of all tensors and

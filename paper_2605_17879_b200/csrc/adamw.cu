@@ -27,7 +27,8 @@ __device__ __forceinline__ double power(double b, int64_t n) {   // b^n by squar
     return r;
 }
 
-// 32 dithering bits of a position: two multiplicative rounds over position and key.  Neighbouring positions and steps
+// 32 dithering bits of a position: two multiplicative rounds over position and key, with multipliers and shifts of the published
+// hash xxHash (32 bits); the positions' upper word is folded in with a multiplier of MurmurHash3.  Neighbouring positions and steps
 // only have to be uncorrelated and each value equally frequent, which the tests count.
 __device__ __forceinline__ uint32_t dither(uint32_t i, uint32_t key) {
     uint32_t h = (i ^ key) * 0x9E3779B1u;

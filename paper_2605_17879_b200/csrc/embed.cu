@@ -16,7 +16,8 @@
 //      The first of these launches also writes zeros to the rows whose token is not in the list (but for those that the SMs
 //      which had nothing to sort have cleared).
 // The grouping of a sum depends on the positions alone.
-// Bound: memory, and above all writing the table (3.9 TB/s at best).  65 536 rows of 2 048 bfloat16 into 131 072: 177 us, of
+// Bound: memory, and above all writing the table (3.9 TB/s at best where it does not fit the second-level cache, as a memset of
+// it does: 139 us for 537 MB).  65 536 rows of 2 048 bfloat16 into 131 072: 177 us, of
 // which 136 are step 2's first launch (650 MB) and 25 the sort.
 #include "train_ops.h"
 
@@ -693,11 +694,15 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
     s.digits = (bits + kDigitBits - 1) / kDigitBits;
     int at = 0;      // which of the two orders holds the result
     cudaError_t e;
-    // Writing the table, at 3.9 TB/s as a memset does, is what bounds the whole, and sorting does not use memory.  So other CTAs
-    // write zeros to the last rows meanwhile; rows whose token occurs are written again
-    // later.  What is left is cleared beside the first sums, or, for short lists, whose few reads would wait behind the writes,
-    // beside the last ones.  5 003 x 1 001 into 32 001 rows of float32: 45 us (with another sort: 48 so, 52 with the rest beside
-    // the first sums, 62 without a head start).
+    // Writing the table is what bounds the whole (a memset writes 537 MB at 3.9 TB/s; 128 MB, which the second-level cache takes
+    // up in part, at 6.2), and sorting does not use memory.  So other CTAs write zeros to the last rows meanwhile; rows whose
+    // token occurs are written again later.  What is left is cleared beside the first sums, or, for short lists, whose few reads
+    // would wait behind the writes, beside the last ones.  5 003 x 1 001 into 32 001 rows of float32: 45 us (with another sort:
+    // 48 so, 52 with the rest beside the first sums, 62 without a head start).  The head start does not pay everywhere, us with
+    // and without it (us, by tokens): 8 000 x 2 048 bfloat16: 16: 10.2, 8.8; 1 100: 21.3, 24.8; 8 000: 40, 37.
+    // 32 001 x 1 001 float32: 16: 22.6, 23.2; 1 100: 43, 40; 8 000: 52, 56; 65 536: 127, 131.  131 072 x 2 048 bfloat16:
+    // 1 100: 118, 106; 8 000: 124, 119; 8 200: 132, 137; 65 536: 177, 183.  Bytes in proportion to the tokens (8 KB each) win 10 %
+    // in the last table for 1 100 to 3 000 tokens and lose 20 % in the first and 10 % for 5 003 in the second.
     const int64_t sms = sm_count(), row_bytes = a.width * (int64_t)dtype_bytes(dtype);
     const bool is_short = a.n <= kShort;
     const int64_t spare = is_short ? sms : sms - L.tiles, launches = is_short ? 1 : 2 * s.digits;

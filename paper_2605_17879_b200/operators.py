@@ -5,6 +5,9 @@ They are the load of a node sweep (sweep_run.py) and ordinary operators besides.
 guard.py: PyTorch supplies device memory and the current stream, every step runs in the library's kernels, and nothing is
 recorded for autograd: a gradient is a call of its own.
 
+Tensors that a call writes (entries of `out`, AdamW's parameters, copies and states) count as changed in place for autograd.
+Calls may come from several threads, each with outputs and workspaces of its own; the interpreter lock is free meanwhile.
+
 Errors in data (a token outside its table) cannot be raised by the call that meets them without waiting for the GPU: they
 are kept in a status word per device, which sync_status() reads and clears, or in the uint32 tensor that the caller passes
 as out["status"].  The first call on a device makes that word and waits for it: make it before capturing a graph.
