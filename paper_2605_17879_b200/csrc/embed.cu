@@ -698,7 +698,7 @@ cudaError_t launch_embed_grad(const EmbedGradArgs &a, int dtype, cudaStream_t st
     // up in part, at 6.2), and sorting does not use memory.  So other CTAs write zeros to the last rows meanwhile; rows whose
     // token occurs are written again later.  What is left is cleared beside the first sums, or, for short lists, whose few reads
     // would wait behind the writes, beside the last ones.  5 003 x 1 001 into 32 001 rows of float32: 45 us (with another sort:
-    // 48 so, 52 with the rest beside the first sums, 62 without a head start).  The head start does not pay everywhere, us with
+    // 48 so, 52 with the rest beside the first sums, 62 without a head start).  The head start does not pay everywhere; with
     // and without it (us, by tokens): 8 000 x 2 048 bfloat16: 16: 10.2, 8.8; 1 100: 21.3, 24.8; 8 000: 40, 37.
     // 32 001 x 1 001 float32: 16: 22.6, 23.2; 1 100: 43, 40; 8 000: 52, 56; 65 536: 127, 131.  131 072 x 2 048 bfloat16:
     // 1 100: 118, 106; 8 000: 124, 119; 8 200: 132, 137; 65 536: 177, 183.  Bytes in proportion to the tokens (8 KB each) win 10 %
