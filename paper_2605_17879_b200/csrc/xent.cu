@@ -6,15 +6,16 @@
 // All four products run on the tensor cores in one kernel frame (product_kernel): pairs of CTAs take tiles of 256 x 256, each
 // CTA loads its half of either operand by TMA, one thread issues tcgen05.mma into the TMEM of both, and eight warps a CTA
 // read the finished accumulator while the next one is filled.  Single CTAs with tiles of 128 x 256 load half as much again
-// per product and were bound by that (4 096 x 1 024 x 65 536 forward 565 us a pass, 512 with pairs, before later steps).  What differs is the last
-// step on an accumulator: the logits' largest value and sum of exponentials per row (the forward pass), G in 16 bits (the
-// backward pass computes the logits again, a piece of the vocabulary at a time), or a gradient.
+// per product and were bound by that (4 096 x 1 024 x 65 536 forward 565 us a pass, 512 with pairs, before later steps).  What
+// differs is the last step on an accumulator: the logits' largest value and sum of exponentials per row (the forward pass), G
+// in 16 bits (the backward pass computes the logits again, a piece of the vocabulary at a time), or a gradient.
 //
 // Bound: the tensor cores, 2 N V D operations per product, but for few rows, where reading w once is what takes the time.
 // The forward product of 4 096 x 1 024 x 65 536 alone takes 328 us, 1 677 TFLOP/s (tensor cores busy 89 % of the cycles); pass
 // after pass 414 to 434 us, since the power limit lowers the clock, as it does for all large sizes (8 192 x 4 096 x 131 072
-// with gradients, four products: 28 to 30 ms, 1 170 to 1 250 TFLOP/s).  The reading warps share the shared-memory pipe with the operands, so what they do to memory
-// counts: an array that the compiler put there, and rows of results stored 16 bytes a lane instead of by TMA, cost 70 us.
+// with gradients, four products: 28 to 30 ms, 1 170 to 1 250 TFLOP/s).  The reading warps share the shared-memory pipe with
+// the operands, so what they do to memory counts: an array that the compiler put there, and rows of results stored 16 bytes a
+// lane instead of by TMA, cost 70 us.
 //
 // Rounding: G is held in the inputs' type, since the tensor cores take both operands in one type; each value is off by at
 // most half a step (relative), as independent of its neighbours as the outputs' own rounding.  It is held relative to the
@@ -898,8 +899,9 @@ struct XentLayout {
 };
 
 // What G of one piece of the vocabulary may take, unless the narrowest piece, a tile of 256 entries, takes more: 512 bytes a
-// row, which is more from 2^20 rows on (2^26 rows, the most there may be: 34 GB).  More pieces cost more passes over dx's partial sums (0.3 GB a piece for
-// 8 192 x 4 096, some 50 us beside 7 ms of products); this is a quarter of the 16-bit logits of 8 192 rows and 131 072 entries.
+// row, which is more from 2^20 rows on (2^26 rows, the most there may be: 34 GB).  More pieces cost more passes over dx's
+// partial sums (0.3 GB a piece for 8 192 x 4 096, some 50 us beside 7 ms of products); this is a quarter of the 16-bit logits
+// of 8 192 rows and 131 072 entries.
 constexpr int64_t kPieceBytes = 512ll << 20;
 
 XentLayout layout(int64_t rows, int64_t width, int64_t vocab, bool grads) {

@@ -249,3 +249,52 @@ def test_adamw_steps_elsewhere_behind_its_making(ops):
         opt.step(1e-2)
     graph.replay()
     assert opt.steps() == 1
+
+
+def test_threads_call_at_the_same_time(ops):
+    """Native calls run without the interpreter lock: threads on streams of their own get their own results and their own
+    errors."""
+    from concurrent.futures import ThreadPoolExecutor
+    g = gen(21)
+    shapes = [(200, 64, 500), (60, 512, 3000), (300, 1032, 700), (1000, 72, 257)]
+    jobs = []
+    for n, d, v in shapes:
+        x = torch.randn(n, d, generator=g, device="cuda").bfloat16()
+        w = (torch.randn(v, d, generator=g, device="cuda") * (2 / d ** 0.5)).bfloat16()
+        t = torch.randint(0, v, (n,), generator=g, device="cuda")
+        jobs.append((x, w, t, torch.full((1,), 1.0 / n, device="cuda")))
+
+    def run(x, w, t, one):
+        out = ops.linear_xent(x, w, t)
+        back = ops.linear_xent_grad(x, w, t, out["lse"], one)
+        rows = ops.embed(t, w)["out"]
+        return [out["loss"], back["dx"], back["dw"], rows, ops.embed_grad(rows, t, len(w))["dtable"]]
+    want = [run(*job) for job in jobs]
+    torch.cuda.synchronize()
+
+    def worker(k):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                got = run(*jobs[k])
+                with pytest.raises(ops.GuardError, match="width a multiple of 8" if k % 2 else "padding_idx"):
+                    if k % 2:
+                        ops.linear_xent(jobs[k][0][:, :12].contiguous(), jobs[k][1][:, :12].contiguous(), jobs[k][2])
+                    else:
+                        ops.embed_grad(got[3], jobs[k][2], len(jobs[k][1]), padding_idx=-7)
+                assert all(torch.equal(a, b) for a, b in zip(got, want[k]))
+        return True
+    with ThreadPoolExecutor(len(jobs)) as pool:
+        assert all(pool.map(worker, range(len(jobs))))
+    ops.sync_status()
+
+
+def test_outputs_have_no_history(ops):
+    """Gradients are calls of their own: nothing is recorded, also where inputs require gradients."""
+    g = gen(22)
+    w = torch.randn(16, 8, generator=g, device="cuda").bfloat16().requires_grad_()
+    x = torch.randn(4, 8, generator=g, device="cuda").bfloat16().requires_grad_()
+    t = torch.tensor([1, 5, 5, 2], device="cuda")
+    out = ops.linear_xent(x, w, t)
+    back = ops.linear_xent_grad(x, w, t, out["lse"], torch.ones(1, device="cuda"))
+    for y in (*out.values(), *back.values(), *ops.embed(t, w).values(), *ops.embed_grad(x, t, 16).values()):
+        assert not y.requires_grad and y.grad_fn is None
