@@ -56,6 +56,28 @@ def test_a_certain_target_is_left_alone(ops, dtype, d, far):
     assert (G.abs() <= tol).all(), (float((G.abs() / tol).max()), float(G.mean()))
 
 
+@pytest.mark.parametrize("n", [100, 500])
+def test_rows_that_move_keep_their_logits(ops, n):
+    """With rows ignored the backward pass finds a row elsewhere in its tile than the forward pass did (100 rows, taken as they
+    are there), or both find it elsewhere than without: the same bits."""
+    d, v = 2056, 700
+    g = gen(n)
+    x = torch.randn(n, d, generator=g, device="cuda").bfloat16()
+    w = (torch.randn(v, d, generator=g, device="cuda") * (2 / math.sqrt(d))).bfloat16()
+    t = torch.randint(0, v, (n,), generator=g, device="cuda")
+    some = torch.where(torch.arange(n, device="cuda") % 3 == 0, -100, t)
+    one = torch.ones(1, device="cuda")
+    full, part = ops.linear_xent(x, w, t), ops.linear_xent(x, w, some)
+    keep = some >= 0
+    assert torch.equal(full["loss"][keep], part["loss"][keep]) and torch.equal(full["lse"][keep], part["lse"][keep])
+    # (dx takes all of the row's G, and its split goes by the number of tiles, which is the same)
+    a, b = ops.linear_xent_grad(x, w, t, full["lse"], one)["dx"], ops.linear_xent_grad(x, w, some, part["lse"], one)["dx"]
+    if n == 100:
+        assert torch.equal(a[keep], b[keep])
+    else:                                                  # two row tiles against three: another grouping of float32 sums
+        assert ((a[keep].double() - b[keep].double()).abs() <= 2 * HALF[torch.bfloat16] * a[keep].double().abs() + 2.0 ** -20).all()
+
+
 def one_signed(seed, n, d, v, dtype, sx, sw):
     """x of either sign and w positive, small logits; every target is entry 0, whose row of w is zero: all terms of dx are
     positive."""
