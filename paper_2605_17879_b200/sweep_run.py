@@ -10,7 +10,7 @@ with the library's own operators (operators.py).  Its parts load what a job's st
 not: irregular reads of the table (embed), the tensor cores under the power limit (loss and gradients), a sort and sums over
 frequent tokens (embed_grad), and a stream over all of parameters and states (AdamW).  Every part is deterministic, so GPUs
 that start from the same seed must report the same losses, bit for bit; one that does not computes wrong results and fails.
-So does one whose load raises an error; the others are judged without it.  The command prints the verdict as one line of JSON
+So does one whose load raises an error; the others are qualified without it.  The command prints the verdict as one line of JSON
 and returns 1 where a load failed or results disagree.
 
     python -m paper_2605_17879_b200.sweep_run                                         one GPU
@@ -125,7 +125,7 @@ def agreement(losses: torch.Tensor) -> List[Optional[bool]]:
     return [r == common for r in rows] if 2 * count > len(rows) else [None] * len(rows)
 
 
-def verdict(rows: torch.Tensor, losses: torch.Tensor, failed: Sequence[bool], gpus_per_node: int, judge=qualify) -> Dict[str, object]:
+def verdict(rows: torch.Tensor, losses: torch.Tensor, failed: Sequence[bool], gpus_per_node: int, qualifier=qualify) -> Dict[str, object]:
     """What the fleet's results say.  rows [gpus, reps, 4], losses [gpus, reps], failed: GPUs whose load raised an error, whose
     results say nothing.  Those fail; the others are qualified against one another, and fail too where they computed other
     losses than the majority.  A node passes when all its GPUs pass."""
@@ -134,7 +134,7 @@ def verdict(rows: torch.Tensor, losses: torch.Tensor, failed: Sequence[bool], gp
     medians, fail_mask, same = [None] * gpus, [None] * gpus, [None] * gpus
     gpu_pass = [0] * gpus
     if good:
-        out = judge(rows[good], len(good), 1)
+        out = qualifier(rows[good], len(good), 1)
         equal = agreement(losses[good])
         for k, g in enumerate(good):
             medians[g] = dict(zip(METRICS, [round(float(x), 3) for x in out["gpu_med"][k]]))
@@ -145,7 +145,7 @@ def verdict(rows: torch.Tensor, losses: torch.Tensor, failed: Sequence[bool], gp
             "same_results": same, "load_failed": [bool(f) for f in failed], "last_loss": float(losses[good[0], -1]) if good else None}
 
 
-def sweep(make, reps: int, gpus_per_node: int, judge=qualify) -> Tuple[Optional[Dict[str, object]], int]:
+def sweep(make, reps: int, gpus_per_node: int, qualifier=qualify) -> Tuple[Optional[Dict[str, object]], int]:
     """Runs the load make() on this rank and collects every rank's results on the host, where a GPU that failed its load can
     still report.  Returns the verdict on the first rank whose load ran (None on the others), and 1 where this rank's load
     failed or the results that were collected disagree."""
@@ -169,7 +169,7 @@ def sweep(make, reps: int, gpus_per_node: int, judge=qualify) -> Tuple[Optional[
     S, losses = gd.gather(rows), gd.gather(loss)
     if rank != (failed.index(False) if False in failed else 0):
         return None, int(error is not None)
-    report = verdict(S, losses, failed, gpus_per_node, judge)
+    report = verdict(S, losses, failed, gpus_per_node, qualifier)
     agree = all(report["same_results"][g] is True for g in range(len(failed)) if not failed[g])
     return report, int(error is not None or not agree)
 

@@ -51,7 +51,7 @@ def test_verdict():
     got = sweep_run.verdict(rows, wrong, [False] * 4, 2, passes)
     assert got["gpu_pass"] == [1, 1, 0, 1] and got["node_pass"] == [1, 0] and got["same_results"] == [True, True, False, True]
     broken = rows.clone()
-    broken[0] = math.nan                                           # its load failed: the others are judged without it
+    broken[0] = math.nan                                           # its load failed: the others are qualified without it
     got = sweep_run.verdict(broken, losses, [True, False, False, False], 2, passes)
     assert got["gpu_pass"] == [0, 1, 1, 1] and got["node_pass"] == [0, 1] and got["medians"][0] is None and got["same_results"][0] is None
     got = sweep_run.verdict(broken, losses, [True] * 4, 4, passes)
